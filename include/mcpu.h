@@ -78,7 +78,9 @@ enum {
   MCPU_DEVERR_PLAN = 8,   /* device seq_lens / cu_q disagree with the host copies */
   MCPU_DEVERR_MXFP4 = 16, /* an MXFP4 block scale outside [2, 252]: scaled values would not be
                              normal bfloat16; that block contributed zero */
-  MCPU_DEVERR_TOKEN = 32  /* a token id outside [0, vocab) (embed_tokens); its row was zeroed */
+  MCPU_DEVERR_TOKEN = 32, /* a token id outside [0, vocab) (embed_tokens); its row was zeroed */
+  MCPU_DEVERR_TREE = 64   /* a tree's parent outside [-1, own index), counted as -1, or a path that does
+                             not ascend inside its tree, whose sequence was left as it was */
 };
 
 /* Layer configuration (host struct, by value semantics). Paper: the policy
@@ -214,9 +216,39 @@ int32_t kv_pool_free_pages(const mcpu_kv_pool* pool);
  * ascending order of the free list, lowest first. */
 int kv_pages_alloc(mcpu_kv_pool* pool, int32_t n, int32_t* out_ids);
 /* Return n pages (a finished trajectory, or sliding-window pages left behind
- * the window). MCPU_EINVAL, freeing nothing, if any id is out
- * of range, not allocated, or repeated. */
+ * the window): each loses one holder, and is free again once it has none.
+ * MCPU_EINVAL, freeing nothing, if any id is out of range, not allocated, or
+ * repeated. */
 int kv_pages_free(mcpu_kv_pool* pool, int32_t n, const int32_t* ids);
+
+/* Sharing and copying pages. A group of trajectories starts from one prompt
+ * (the policy update compares the members of a group, Sec. 4), so the pages
+ * that the prompt filled are held by every member instead of being computed
+ * and stored once for each. A shared page is only read: a member that goes on
+ * writing inside the prompt's partly filled last page takes a page of its own
+ * and copies that one.
+ *
+ * kv_pages_share adds a holder to each of n allocated pages (one per
+ * occurrence: an id may repeat). MCPU_EINVAL, adding nothing, if an id is out of
+ * range or not allocated. kv_page_holders: the number of holders (0: free), or
+ * MCPU_EINVAL. */
+int kv_pages_share(mcpu_kv_pool* pool, int32_t n, const int32_t* ids);
+int32_t kv_page_holders(const mcpu_kv_pool* pool, int32_t id);
+
+/* Copy whole pages, K and V, in every layer whose page table uses the same ids:
+ * page src[i] -> page dst[i], i < n, in each of the n_pools pools (1 to
+ * MCPU_MAX_POOLS distinct handles of the same KV heads, head dim and dtype), in
+ * one launch.
+ *  src, dst: device int32 [n]; host_src, host_dst: host copies of the same
+ *  arrays. A source may repeat; MCPU_EINVAL, copying nothing, if an id lies
+ *  outside the smallest pool, a destination repeats, or a destination is a
+ *  source. Ids outside the pools on the device alone set MCPU_DEVERR_PAGE and are
+ *  skipped; that the device's destinations are distinct is the caller's duty.
+ *  workspace: at least 256 bytes (error word). */
+enum { MCPU_MAX_POOLS = 64 };
+int kv_pages_copy(mcpu_kv_pool* const* pools, int32_t n_pools, int32_t n, const int32_t* src, const int32_t* dst,
+                  const int32_t* host_src, const int32_t* host_dst, void* workspace, size_t ws_bytes,
+                  hipStream_t stream);
 
 /* Write new keys and values into the cache (the append of a step; Sec. 1 and
  * Sec. 3.2: generated tokens and tool observations join the context).
@@ -253,6 +285,64 @@ int paged_attention(const mcpu_layer_cfg* cfg, const float* sinks, mcpu_kv_pool*
                     const int32_t* seq_lens, const int32_t* cu_q, const int32_t* host_seq_lens,
                     const int32_t* host_cu_q, const void* q, void* o, void* workspace,
                     size_t ws_bytes, hipStream_t stream);
+
+/* ---- Trees of drafted tokens ------------------------------------------ */
+/* Several drafted continuations of a sequence are verified in one step of the
+ * Run stage's generation (Sec. 3.2): they form a tree whose nodes are the new
+ * tokens of the step. A draw depends only on (seed, sequence, position)
+ * (lm_head_sample), so the drafted tokens that equal the draws of the tokens
+ * before them are exactly the tokens that a token-by-token step would have
+ * produced.
+ *
+ * The tree of sequence b is the rows cu_q[b] .. cu_q[b + 1] - 1 of the step: n =
+ * 0 to MCPU_TREE_MAX_NODES nodes. Node i's K and V are written to cache position
+ * seq_lens[b] + i (kv_pages_append, or the layer itself). parents[cu_q[b] + i] is
+ * the node before it, an index in [0, i), or -1 if that is the last committed
+ * token. depth(i) = 0 for parent -1, else depth(parent) + 1; the node stands at
+ * position p_i = seq_lens[b] + depth(i), by which its q and k are rotated. */
+enum { MCPU_TREE_MAX_NODES = 64 };
+
+/* Attention of a step's tree nodes, already appended: node i attends to the
+ * committed keys and to its ancestors and itself, in a window w > 0 to those of
+ * them at positions above p_i - w. Formula, sinks, types and layouts as for
+ * paged_attention; a node whose keys all lie on missing pages gives zeros when
+ * there is no sink. Cache contents that no node of the tree sees (slots behind
+ * the tree, stale ones, other branches) have no effect on a node, whatever they
+ * hold.
+ *  cu_q (device) and host_cu_q are required, as are host_seq_lens; parents:
+ *  device int32 [n_tokens]. Each tree has up to MCPU_TREE_MAX_NODES nodes, else
+ *  MCPU_EUNSUPPORTED. Rows of q and o outside the trees do not exist. */
+size_t tree_attention_workspace_size(const mcpu_layer_cfg* cfg, int32_t max_batch, int32_t max_tokens);
+int tree_attention(const mcpu_layer_cfg* cfg, const float* sinks, mcpu_kv_pool* pool, int32_t batch,
+                   const int32_t* page_table, int32_t max_pages, const int32_t* seq_lens, const int32_t* cu_q,
+                   const int32_t* parents, const int32_t* host_seq_lens, const int32_t* host_cu_q, const void* q,
+                   void* o, void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* The path that the draws confirm. Node 0 is the tree's root, a token that is
+ * certain (the last one drawn); draft[t] is the id of row t's token, sampled[t]
+ * the id drawn after it. From the root on, the path goes to the lowest child
+ * whose draft equals the draw at its parent, until there is none.
+ *  batch trees over n_tokens rows; cu_q [batch + 1], parents, draft, sampled
+ *  [n_tokens] device int32. Outputs, device int32: path [n_tokens], for each tree
+ *  the nodes of its path in order from the root, then -1; n_path [batch] their
+ *  number (0 for an empty tree); next [batch] the draw at the path's last node
+ *  (-1 for an empty tree). workspace: at least 256 bytes (error word). */
+int tree_accept(int32_t batch, int32_t n_tokens, const int32_t* cu_q, const int32_t* parents, const int32_t* draft,
+                const int32_t* sampled, int32_t* path, int32_t* n_path, int32_t* next, void* workspace,
+                size_t ws_bytes, hipStream_t stream);
+
+/* Keep an accepted path: the K and V at positions seq_lens[b] + path[cu_q[b] + i]
+ * move to seq_lens[b] + i, i < n_path[b], in each of the n_pools pools (as for
+ * kv_pages_copy) that page_table belongs to, in one launch; every other slot is
+ * left as it was. The caller then advances seq_lens by n_path. path must ascend
+ * (it does from tree_accept): else MCPU_DEVERR_TREE. A page missing on either side
+ * sets MCPU_DEVERR_PAGE and that token is not moved.
+ *  page_table [batch, max_pages], seq_lens [batch], cu_q [batch + 1], path
+ *  [n_tokens], n_path [batch]: device int32; the sequences' pages from position
+ *  seq_lens on are not shared. workspace: at least 256 bytes (error word). */
+int kv_tree_commit(mcpu_kv_pool* const* pools, int32_t n_pools, int32_t batch, const int32_t* page_table,
+                   int32_t max_pages, const int32_t* seq_lens, const int32_t* cu_q, int32_t n_tokens,
+                   const int32_t* path, const int32_t* n_path, void* workspace, size_t ws_bytes, hipStream_t stream);
 
 /* MoE sub-block on the residual stream (the policy's mixture-of-experts
  * feed-forward, Sec. 4): h, out [n_tokens, H] fp32 (may alias).
@@ -410,7 +500,13 @@ enum {
   MCPU_KERNEL_KV_APPEND = 11,
   MCPU_KERNEL_ATTN_PREFILL = 12, /* chunked-prefill attention */
   MCPU_KERNEL_LM_HEAD = 13,      /* vocabulary projection + sampling summaries */
-  MCPU_KERNEL_COUNT = 14
+  MCPU_KERNEL_TREE_PLAN = 14,
+  MCPU_KERNEL_TREE_ATTN = 15,    /* tree attention, a split each */
+  MCPU_KERNEL_TREE_COMBINE = 16,
+  MCPU_KERNEL_TREE_ACCEPT = 17,
+  MCPU_KERNEL_TREE_COMMIT = 18,
+  MCPU_KERNEL_PAGES_COPY = 19,
+  MCPU_KERNEL_COUNT = 20
 };
 int mcpu_timing_start(int kernel, int n);
 int mcpu_timing_read(int kernel, float* ms, int n, int* n_recorded);

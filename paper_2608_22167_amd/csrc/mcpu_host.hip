@@ -7,7 +7,9 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <memory>
 #include <mutex>
+#include <new>
 #include <set>
 #include <string>
 #include <vector>
@@ -15,6 +17,7 @@
 #include "../../include/mcpu.h"
 #include "kernels.h"
 #include "kernels_lm.h"
+#include "kernels_tree.h"
 
 using namespace mcpu;
 
@@ -378,7 +381,7 @@ struct mcpu_kv_pool {
   void* k;
   void* v;
   std::set<int32_t> free_ids;
-  std::vector<uint8_t> in_use;
+  std::vector<int32_t> holders;  // per page; 0: free
 };
 
 namespace {
@@ -429,6 +432,129 @@ int run_attention(const mcpu_layer_cfg* c, const float* sinks, mcpu_kv_pool* poo
 bool same_shape(const mcpu_layer_cfg* a, const mcpu_layer_cfg* b) {
   return a->n_kv_heads == b->n_kv_heads && a->head_dim == b->head_dim && a->dtype == b->dtype;
 }
+
+// The device pools of handles that share one page-id space; *n_pages: the smallest.
+static_assert(MAX_POOLS == MCPU_MAX_POOLS && TREE_MAX_NODES == MCPU_TREE_MAX_NODES, "limits of mcpu.h");
+int collect_pools(mcpu_kv_pool* const* pools, int32_t n_pools, PoolSet* out, int* n_pages) {
+  if (!pools || n_pools <= 0) return fail(MCPU_EINVAL, "n_pools %d", n_pools);
+  if (n_pools > MAX_POOLS) return fail(MCPU_EUNSUPPORTED, "n_pools %d (at most %d)", n_pools, MAX_POOLS);
+  for (int i = 0; i < n_pools; ++i) {
+    if (!pools[i] || !same_shape(&pools[i]->cfg, &pools[0]->cfg))
+      return fail(MCPU_EINVAL, "pool %d missing or of another shape", i);
+    for (int j = 0; j < i; ++j)
+      if (pools[j] == pools[i] || pools[j]->k == pools[i]->k || pools[j]->v == pools[i]->v)
+        return fail(MCPU_EINVAL, "pools %d and %d are the same", j, i);
+    out->k[i] = pools[i]->k;
+    out->v[i] = pools[i]->v;
+    *n_pages = i ? std::min(*n_pages, pools[i]->n_pages) : pools[i]->n_pages;
+  }
+  return MCPU_OK;
+}
+
+// ---- trees of drafted tokens -------------------------------------------------
+
+constexpr int TREE_EXTRA_ROWS = 4096;  // partial rows beyond one per node that the workspace holds
+
+struct TreePlanHost {
+  int n_tokens = 0, max_nodes = 0, max_pos = 0;
+  int pps = 0, n_items = 0, n_rows = 0;
+};
+
+// Validate host positions and choose the pages per split, so that the splits
+// fill the GPU and their partial rows fit the workspace.
+int plan_tree(const mcpu_layer_cfg* c, int batch, int max_pages, const int32_t* hsl, const int32_t* hcu,
+              TreePlanHost* out) {
+  if (!hsl || !hcu) return fail(MCPU_EINVAL, "host_seq_lens or host_cu_q is NULL");
+  if (hcu[0] != 0) return fail(MCPU_EINVAL, "host_cu_q[0] must be 0");
+  auto pages_of = [&](int b, int n) {
+    const int lo = c->window > 0 ? std::max(0, hsl[b] - c->window + 1) : 0;
+    return (hsl[b] + n - 1) / PAGE_SIZE - lo / PAGE_SIZE + 1;
+  };
+  long long total = 0;
+  for (int b = 0; b < batch; ++b) {
+    const int n = hcu[b + 1] - hcu[b];
+    if (n < 0) return fail(MCPU_EINVAL, "host_cu_q is not non-decreasing at %d", b);
+    if (n > TREE_MAX_NODES) return fail(MCPU_EUNSUPPORTED, "tree %d has %d nodes (at most %d)", b, n, TREE_MAX_NODES);
+    if (hsl[b] < 0) return fail(MCPU_EINVAL, "seq_lens[%d] = %d < 0", b, hsl[b]);
+    if (n == 0) continue;
+    if (((long long)hsl[b] + n - 1) / PAGE_SIZE >= max_pages)
+      return fail(MCPU_EINVAL, "sequence %d position %lld beyond page table width %d", b, (long long)hsl[b] + n - 1, max_pages);
+    out->max_nodes = std::max(out->max_nodes, n);
+    out->max_pos = std::max(out->max_pos, hsl[b] + n - 1);
+    total += pages_of(b, n);
+  }
+  out->n_tokens = hcu[batch];
+  const long long target = std::max<long long>(1, (long long)TARGET_WAVES / c->n_kv_heads);
+  long long pps = std::max<long long>(PPS_MIN, (total + target - 1) / target);
+  for (;; pps *= 2) {
+    long long items = 0, rows = 0;
+    for (int b = 0; b < batch; ++b) {
+      const int n = hcu[b + 1] - hcu[b];
+      if (n == 0) continue;
+      const long long splits = (pages_of(b, n) + pps - 1) / pps;
+      items += splits;
+      if (splits > 1) rows += splits * n;
+    }
+    if (rows > (long long)out->n_tokens + TREE_EXTRA_ROWS) continue;  // ends: one split each leaves no row
+    out->pps = (int)std::min<long long>(pps, INT32_MAX);
+    out->n_items = (int)items;
+    out->n_rows = (int)rows;
+    return MCPU_OK;
+  }
+}
+
+struct TreeBufs {
+  TreeNode* node;
+  TreeItem* item;
+  int32_t* tok_seq;
+  int2* seq_split;
+  float *part_ml, *part_acc;
+};
+
+TreeBufs carve_tree(Carve& cv, const mcpu_layer_cfg* c, int max_batch, int max_tokens) {
+  TreeBufs b;
+  const size_t rows = (size_t)max_tokens + TREE_EXTRA_ROWS;
+  b.node = cv.take<TreeNode>(max_tokens);
+  b.item = cv.take<TreeItem>(rows + max_batch);  // a split has a row at least, a tree without splits is one item
+  b.tok_seq = cv.take<int32_t>(max_tokens);
+  b.seq_split = cv.take<int2>(max_batch);
+  b.part_ml = cv.take<float>(rows * c->n_q_heads * 2);
+  b.part_acc = cv.take<float>(rows * c->n_q_heads * c->head_dim);
+  return b;
+}
+
+int run_tree_attention(const mcpu_layer_cfg* c, const float* sinks, mcpu_kv_pool* pool, int batch,
+                       const int32_t* page_table, int max_pages, const int32_t* seq_lens, const int32_t* cu_q,
+                       const int32_t* parents, const TreePlanHost& ph, const void* q, void* o, const TreeBufs& tb,
+                       int32_t* err, hipStream_t st) {
+  TreePlan pl{};
+  pl.seq_lens = seq_lens; pl.cu_q = cu_q; pl.parents = parents; pl.batch = batch; pl.n_tokens = ph.n_tokens;
+  pl.max_pages = max_pages; pl.window = c->window; pl.pps = ph.pps; pl.n_items = ph.n_items; pl.n_rows = ph.n_rows;
+  pl.node = tb.node; pl.item = tb.item; pl.tok_seq = tb.tok_seq; pl.seq_split = tb.seq_split; pl.err = err;
+  {
+    Timed tm(MCPU_KERNEL_TREE_PLAN, st);
+    HIP_TRY(launch_tree_plan(pl, st));
+  }
+  TreeAttn ta{};
+  ta.q = q; ta.k_pool = pool->k; ta.v_pool = pool->v; ta.page_table = page_table; ta.max_pages = max_pages;
+  ta.n_pages = pool->n_pages; ta.node = tb.node; ta.item = tb.item; ta.batch = batch; ta.n_tokens = ph.n_tokens;
+  ta.n_items = ph.n_items; ta.n_rows = ph.n_rows; ta.max_nodes = ph.max_nodes; ta.hq = c->n_q_heads;
+  ta.hkv = c->n_kv_heads; ta.window = c->window;
+  ta.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c->head_dim));
+  ta.sinks = sinks; ta.part_ml = tb.part_ml; ta.part_acc = tb.part_acc; ta.o = o; ta.err = err;
+  {
+    Timed tm(MCPU_KERNEL_TREE_ATTN, st);
+    HIP_TRY(launch_tree_attn(c->dtype, c->head_dim, ta, st));
+  }
+  if (ph.n_rows == 0) return MCPU_OK;
+  TreeCombine cb{};
+  cb.part_ml = tb.part_ml; cb.part_acc = tb.part_acc; cb.cu_q = cu_q; cb.tok_seq = tb.tok_seq;
+  cb.seq_split = tb.seq_split; cb.sinks = sinks; cb.batch = batch; cb.n_tokens = ph.n_tokens; cb.n_rows = ph.n_rows;
+  cb.hq = c->n_q_heads; cb.o = o;
+  Timed tm(MCPU_KERNEL_TREE_COMBINE, st);
+  HIP_TRY(launch_tree_combine(c->dtype, c->head_dim, cb, st));
+  return MCPU_OK;
+}
 }  // namespace
 
 extern "C" {
@@ -446,7 +572,7 @@ int kv_pool_create(const mcpu_layer_cfg* cfg, int32_t n_pages, void* k_pool, voi
   p->n_pages = n_pages;
   p->k = k_pool;
   p->v = v_pool;
-  p->in_use.assign(n_pages, 0);
+  p->holders.assign(n_pages, 0);
   for (int32_t i = 0; i < n_pages; ++i) p->free_ids.insert(p->free_ids.end(), i);
   *out = p;
   return MCPU_OK;
@@ -466,7 +592,7 @@ int kv_pages_alloc(mcpu_kv_pool* pool, int32_t n, int32_t* out_ids) {
   auto it = pool->free_ids.begin();
   for (int32_t i = 0; i < n; ++i) {
     out_ids[i] = *it;
-    pool->in_use[*it] = 1;
+    pool->holders[*it] = 1;
     it = pool->free_ids.erase(it);
   }
   return MCPU_OK;
@@ -478,15 +604,63 @@ int kv_pages_free(mcpu_kv_pool* pool, int32_t n, const int32_t* ids) {
   for (int32_t i = 0; i < n; ++i) {
     int32_t id = ids[i];
     if (id < 0 || id >= pool->n_pages) return fail(MCPU_EINVAL, "kv_pages_free: id %d out of range", id);
-    if (!pool->in_use[id]) return fail(MCPU_EINVAL, "kv_pages_free: page %d is not allocated", id);
+    if (!pool->holders[id]) return fail(MCPU_EINVAL, "kv_pages_free: page %d is not allocated", id);
     if (seen.empty()) seen.assign(pool->n_pages, 0);
     if (seen[id]) return fail(MCPU_EINVAL, "kv_pages_free: page %d repeated", id);
     seen[id] = 1;
   }
   for (int32_t i = 0; i < n; ++i) {
-    pool->in_use[ids[i]] = 0;
-    pool->free_ids.insert(ids[i]);
+    if (--pool->holders[ids[i]] == 0) pool->free_ids.insert(ids[i]);
   }
+  return MCPU_OK;
+}
+
+int kv_pages_share(mcpu_kv_pool* pool, int32_t n, const int32_t* ids) {
+  if (!pool || (n > 0 && !ids) || n < 0) return fail(MCPU_EINVAL, "kv_pages_share: bad arguments");
+  for (int32_t i = 0; i < n; ++i) {
+    if (ids[i] < 0 || ids[i] >= pool->n_pages) return fail(MCPU_EINVAL, "kv_pages_share: id %d out of range", ids[i]);
+    if (!pool->holders[ids[i]]) return fail(MCPU_EINVAL, "kv_pages_share: page %d is not allocated", ids[i]);
+    if (pool->holders[ids[i]] > INT32_MAX - n) return fail(MCPU_EINVAL, "kv_pages_share: page %d has too many holders", ids[i]);
+  }
+  for (int32_t i = 0; i < n; ++i) ++pool->holders[ids[i]];
+  return MCPU_OK;
+}
+
+int32_t kv_page_holders(const mcpu_kv_pool* pool, int32_t id) {
+  if (!pool || id < 0 || id >= pool->n_pages) return fail(MCPU_EINVAL, "kv_page_holders: bad arguments");
+  return pool->holders[id];
+}
+
+int kv_pages_copy(mcpu_kv_pool* const* pools, int32_t n_pools, int32_t n, const int32_t* src, const int32_t* dst,
+                  const int32_t* host_src, const int32_t* host_dst, void* workspace, size_t ws_bytes,
+                  hipStream_t stream) {
+  PagesCopy a{};
+  int rc = collect_pools(pools, n_pools, &a.pools, &a.n_pages);
+  if (rc) return rc;
+  if (n < 0) return fail(MCPU_EINVAL, "n %d", n);
+  if (n == 0) return MCPU_OK;
+  if (!src || !dst || !host_src || !host_dst || !workspace) return fail(MCPU_EINVAL, "NULL pointer");
+  if (ws_bytes < 256) return fail(MCPU_ENOMEM, "workspace smaller than 256 bytes");
+  // bit sets over the pages: destinations, then sources against them
+  const size_t words = ((size_t)a.n_pages + 63) / 64;
+  std::unique_ptr<uint64_t[]> is_dst(new (std::nothrow) uint64_t[words]());
+  if (!is_dst) return fail(MCPU_ENOMEM, "host allocation failed");
+  for (int32_t i = 0; i < n; ++i) {
+    const int32_t s = host_src[i], d = host_dst[i];
+    if (s < 0 || s >= a.n_pages || d < 0 || d >= a.n_pages)
+      return fail(MCPU_EINVAL, "kv_pages_copy: page %d -> %d outside the pools' %d pages", s, d, a.n_pages);
+    if (is_dst[d / 64] >> (d % 64) & 1) return fail(MCPU_EINVAL, "kv_pages_copy: destination %d repeated", d);
+    is_dst[d / 64] |= 1ull << (d % 64);
+  }
+  for (int32_t i = 0; i < n; ++i)
+    if (is_dst[host_src[i] / 64] >> (host_src[i] % 64) & 1)
+      return fail(MCPU_EINVAL, "kv_pages_copy: page %d is a source and a destination", host_src[i]);
+  const mcpu_layer_cfg& c = pools[0]->cfg;
+  a.n_pools = n_pools; a.n = n; a.src = src; a.dst = dst;
+  a.page_bytes = (int64_t)c.n_kv_heads * PAGE_SIZE * c.head_dim * dtype_bytes(&c);
+  a.err = err_word(workspace);
+  Timed tm(MCPU_KERNEL_PAGES_COPY, stream);
+  HIP_TRY(launch_pages_copy(a, stream));
   return MCPU_OK;
 }
 
@@ -537,6 +711,70 @@ int paged_attention(const mcpu_layer_cfg* cfg, const float* sinks, mcpu_kv_pool*
   AttnBufs ab = carve_attention(cv, cfg, std::max(ph.n_tokens, batch));
   return run_attention(cfg, sinks, pool, batch, page_table, max_pages, seq_lens, cu_q, ph, q, o, ab,
                        err_word(workspace), stream, false);
+}
+
+size_t tree_attention_workspace_size(const mcpu_layer_cfg* cfg, int32_t max_batch, int32_t max_tokens) {
+  if (check_cfg(cfg) || max_batch < 0 || max_tokens < 0) return 0;
+  Carve cv(nullptr);
+  carve_tree(cv, cfg, max_batch, max_tokens);
+  return (cv.off + 255) & ~size_t(255);
+}
+
+int tree_attention(const mcpu_layer_cfg* cfg, const float* sinks, mcpu_kv_pool* pool, int32_t batch,
+                   const int32_t* page_table, int32_t max_pages, const int32_t* seq_lens, const int32_t* cu_q,
+                   const int32_t* parents, const int32_t* host_seq_lens, const int32_t* host_cu_q, const void* q,
+                   void* o, void* workspace, size_t ws_bytes, hipStream_t stream) {
+  int rc = check_cfg(cfg);
+  if (rc) return rc;
+  if (!pool || !same_shape(cfg, &pool->cfg)) return fail(MCPU_EINVAL, "pool missing or of another shape");
+  if (batch <= 0 || max_pages <= 0) return fail(MCPU_EINVAL, "batch %d, max_pages %d", batch, max_pages);
+  if (!page_table || !seq_lens || !cu_q || !workspace) return fail(MCPU_EINVAL, "NULL pointer");
+  TreePlanHost ph;
+  if ((rc = plan_tree(cfg, batch, max_pages, host_seq_lens, host_cu_q, &ph))) return rc;
+  if (ph.n_tokens == 0) return MCPU_OK;
+  if (!parents || !q || !o) return fail(MCPU_EINVAL, "NULL pointer");
+  if ((uintptr_t)q % 16 || (uintptr_t)o % 16) return fail(MCPU_EINVAL, "q and o must be 16-byte aligned");
+  const size_t need = tree_attention_workspace_size(cfg, batch, ph.n_tokens);
+  if (ws_bytes < need) return fail(MCPU_ENOMEM, "workspace %zu bytes < %zu needed", ws_bytes, need);
+  Carve cv(workspace);
+  const TreeBufs tb = carve_tree(cv, cfg, batch, ph.n_tokens);
+  return run_tree_attention(cfg, sinks, pool, batch, page_table, max_pages, seq_lens, cu_q, parents, ph, q, o, tb,
+                            err_word(workspace), stream);
+}
+
+int tree_accept(int32_t batch, int32_t n_tokens, const int32_t* cu_q, const int32_t* parents, const int32_t* draft,
+                const int32_t* sampled, int32_t* path, int32_t* n_path, int32_t* next, void* workspace,
+                size_t ws_bytes, hipStream_t stream) {
+  if (batch < 0 || n_tokens < 0) return fail(MCPU_EINVAL, "batch %d, n_tokens %d", batch, n_tokens);
+  if (batch == 0) return MCPU_OK;
+  if (!cu_q || !n_path || !next || !workspace) return fail(MCPU_EINVAL, "NULL pointer");
+  if (n_tokens > 0 && (!parents || !draft || !sampled || !path)) return fail(MCPU_EINVAL, "NULL pointer");
+  if (ws_bytes < 256) return fail(MCPU_ENOMEM, "workspace smaller than 256 bytes");
+  TreeAccept a{};
+  a.cu_q = cu_q; a.parents = parents; a.draft = draft; a.sampled = sampled; a.batch = batch; a.n_tokens = n_tokens;
+  a.path = path; a.n_path = n_path; a.next = next; a.err = err_word(workspace);
+  Timed tm(MCPU_KERNEL_TREE_ACCEPT, stream);
+  HIP_TRY(launch_tree_accept(a, stream));
+  return MCPU_OK;
+}
+
+int kv_tree_commit(mcpu_kv_pool* const* pools, int32_t n_pools, int32_t batch, const int32_t* page_table,
+                   int32_t max_pages, const int32_t* seq_lens, const int32_t* cu_q, int32_t n_tokens,
+                   const int32_t* path, const int32_t* n_path, void* workspace, size_t ws_bytes, hipStream_t stream) {
+  TreeCommit a{};
+  int rc = collect_pools(pools, n_pools, &a.pools, &a.n_pages);
+  if (rc) return rc;
+  if (batch < 0 || n_tokens < 0 || max_pages <= 0)
+    return fail(MCPU_EINVAL, "batch %d, n_tokens %d, max_pages %d", batch, n_tokens, max_pages);
+  if (batch == 0 || n_tokens == 0) return MCPU_OK;
+  if (!page_table || !seq_lens || !cu_q || !path || !n_path || !workspace) return fail(MCPU_EINVAL, "NULL pointer");
+  if (ws_bytes < 256) return fail(MCPU_ENOMEM, "workspace smaller than 256 bytes");
+  a.n_pools = n_pools; a.hkv = pools[0]->cfg.n_kv_heads; a.page_table = page_table; a.max_pages = max_pages;
+  a.seq_lens = seq_lens; a.cu_q = cu_q; a.path = path; a.n_path = n_path; a.batch = batch; a.n_tokens = n_tokens;
+  a.err = err_word(workspace);
+  Timed tm(MCPU_KERNEL_TREE_COMMIT, stream);
+  HIP_TRY(launch_tree_commit(pools[0]->cfg.dtype, pools[0]->cfg.head_dim, a, stream));
+  return MCPU_OK;
 }
 
 size_t mcpu_packed_weights_bytes(int32_t n_groups, int32_t rows, int32_t cols) {

@@ -29,12 +29,16 @@ EXPORTED = ("mcpu_last_error", "kv_pool_create", "kv_pool_destroy", "kv_pool_fre
             "decode_layer_workspace_size", "decode_layer", "mcpu_check_device_errors",
             "mcpu_timing_start", "mcpu_timing_read", "mcpu_packed_weights_bytes", "mcpu_pack_weights",
             "lm_head_workspace_size", "lm_head_sample", "embed_tokens", "decode_layer_noalloc",
-            "mcpu_mxfp8_quantize", "mcpu_packed_mxfp4_bytes", "mcpu_pack_mxfp4")
+            "mcpu_mxfp8_quantize", "mcpu_packed_mxfp4_bytes", "mcpu_pack_mxfp4",
+            "kv_pages_share", "kv_page_holders", "kv_pages_copy", "tree_attention_workspace_size", "tree_attention",
+            "tree_accept", "kv_tree_commit")
 NOALLOC_SCRATCH_BYTES = 128 << 20  # the static scratch of decode_layer_noalloc, per GPU
 
 KERNELS = ("attn_plan", "rmsnorm", "qkv", "attn_split", "attn_combine", "oproj", "router", "permute",
-           "expert_gu", "expert_down", "moe_combine", "kv_append", "attn_prefill", "lm_head")
-DEVERR_TOKEN = 32
+           "expert_gu", "expert_down", "moe_combine", "kv_append", "attn_prefill", "lm_head",
+           "tree_plan", "tree_attn", "tree_combine", "tree_accept", "tree_commit", "pages_copy")
+DEVERR_TOKEN, DEVERR_TREE = 32, 64
+TREE_MAX_NODES, MAX_POOLS = 64, 64
 
 
 class McpuError(RuntimeError):
@@ -110,6 +114,15 @@ def lib():
         L.mcpu_packed_mxfp4_bytes.argtypes = [i32, i32, i32]
         L.mcpu_packed_mxfp4_bytes.restype = sz
         L.mcpu_pack_mxfp4.argtypes = [vp, vp, vp, i32, i32, i32, vp]
+        L.kv_pages_share.argtypes = [vp, i32, vp]
+        L.kv_page_holders.argtypes = [vp, i32]
+        L.kv_page_holders.restype = i32
+        L.kv_pages_copy.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.tree_attention_workspace_size.argtypes = [vp, i32, i32]
+        L.tree_attention_workspace_size.restype = sz
+        L.tree_attention.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.tree_accept.argtypes = [i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.kv_tree_commit.argtypes = [vp, i32, i32, vp, i32, vp, vp, i32, vp, vp, vp, sz, vp]
         L.mcpu_timing_start.argtypes = [i32, i32]
         L.mcpu_timing_read.argtypes = [i32, vp, i32, i32p]
         _LIB = L
@@ -274,6 +287,33 @@ def kv_pages_append(pool: KVPool, page_table, seq_lens, cu_q, k_new, v_new, work
                                  _stream(stream)))
 
 
+def kv_pages_share(pool: KVPool, ids) -> None:
+    """Add a holder to each page (kv_pages_free drops one)."""
+    ids = _host_i32(ids)
+    _check(lib().kv_pages_share(pool.handle, len(ids), _ptr(ids) if len(ids) else None))
+
+
+def kv_page_holders(pool: KVPool, page: int) -> int:
+    n = lib().kv_page_holders(pool.handle, page)
+    if n < 0:
+        _check(n)
+    return n
+
+
+def _handles(pools):
+    return (ctypes.c_void_p * len(pools))(*[p.handle for p in pools])
+
+
+def kv_pages_copy(pools, src, dst, host_src, host_dst, workspace, stream=None):
+    """Page src[i] -> page dst[i] in every pool of `pools` (layers that share the ids)."""
+    hs, hd = _host_i32(host_src), _host_i32(host_dst)
+    n = int(src.shape[0])
+    if len(hs) != n or len(hd) != n or int(dst.shape[0]) != n:
+        raise McpuError(MCPU_EINVAL, "src, dst and their host copies differ in length")
+    _check(lib().kv_pages_copy(_handles(pools), len(pools), n, _ptr(src), _ptr(dst), _ptr(hs), _ptr(hd),
+                               _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
 def workspace(nbytes: int, device="cuda") -> torch.Tensor:
     """Zero-filled, 256-byte aligned device workspace."""
     return torch.zeros(max(nbytes, 256), dtype=torch.uint8, device=device)
@@ -292,6 +332,35 @@ def paged_attention(shape, sinks, pool: KVPool, page_table, seq_lens, cu_q, host
                                  _ptr(page_table), int(page_table.shape[1]), _ptr(seq_lens), _ptr(cu_q),
                                  _ptr(hs), _ptr(hc), _ptr(q), _ptr(o), _ptr(workspace),
                                  workspace.numel(), _stream(stream)))
+
+
+def tree_attention_workspace_size(shape, max_batch, max_tokens) -> int:
+    cfg = make_cfg(shape)
+    return lib().tree_attention_workspace_size(ctypes.byref(cfg), max_batch, max_tokens)
+
+
+def tree_attention(shape, sinks, pool: KVPool, page_table, seq_lens, cu_q, parents, host_seq_lens, host_cu_q,
+                   q, o, workspace, stream=None):
+    cfg = make_cfg(shape)
+    hs, hc = _host_i32(host_seq_lens), _host_i32(host_cu_q)
+    _check(lib().tree_attention(ctypes.byref(cfg), _ptr(sinks), pool.handle, int(seq_lens.shape[0]),
+                                _ptr(page_table), int(page_table.shape[1]), _ptr(seq_lens), _ptr(cu_q),
+                                _ptr(parents), _ptr(hs), _ptr(hc), _ptr(q), _ptr(o), _ptr(workspace),
+                                workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def tree_accept(cu_q, parents, draft, sampled, path, n_path, next_tokens, workspace, stream=None):
+    _check(lib().tree_accept(int(cu_q.shape[0]) - 1, int(parents.shape[0]), _ptr(cu_q), _ptr(parents), _ptr(draft),
+                             _ptr(sampled), _ptr(path), _ptr(n_path), _ptr(next_tokens), _ptr(workspace),
+                             workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def kv_tree_commit(pools, page_table, seq_lens, cu_q, path, n_path, workspace, stream=None):
+    """Keep an accepted path in every pool of `pools` (the layers that page_table belongs to)."""
+    _check(lib().kv_tree_commit(_handles(pools), len(pools), int(seq_lens.shape[0]), _ptr(page_table),
+                                int(page_table.shape[1]), _ptr(seq_lens), _ptr(cu_q), int(path.shape[0]), _ptr(path),
+                                _ptr(n_path), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                _stream(stream)))
 
 
 def moe_forward_workspace_size(shape, max_tokens) -> int:
