@@ -9,6 +9,8 @@
 //   plan     splits each tree's page range, and finds every node's ancestors
 //   attend   one split of one tree and KV head: running maximum, sum and values
 //   combine  merges the splits of trees that have several, with the sink
+#include <type_traits>
+
 #include "device.h"
 #include "kernels_tree.h"
 
@@ -337,8 +339,383 @@ static hipError_t tree_attn_impl(const TreeAttn& p, hipStream_t s) {
   return hipGetLastError();
 }
 
+// ---------------------------------------------------------------------------
+// attend, bf16 with head dim 64: 64 columns per wavefront
+// ---------------------------------------------------------------------------
+
+// A workgroup of NC wavefronts owns one split of one tree and KV head; each
+// wavefront holds 64 columns, two tiles of 32. The pages go straight to LDS, two
+// (32 keys) a step through TRS stages, once for all NC wavefronts. Per step a
+// wavefront forms S^T = K Q^T as a 32 x 32 tile per 32 columns and accumulates
+// O^T += V^T P^T from it: lane l holds column l % 32 and, with h = l / 32, keys
+// 8 q + 4 h + r (element 4 q + r), which is the value product's operand order.
+// The scores of step s + 1 are formed beside the weights of step s.
+//
+// The maximum of a column is raised only when a lane's share of a step's weights
+// would pass 2^8, so that most steps have no cross-lane step and no rescale.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) void* lds_void_t;
+
+template <int NC, int TRS>
+__global__ __launch_bounds__(64 * NC, 2) void tree_attn_wide_kernel(TreeAttn P, int tiles) {
+  constexpr int D = 64, PE = PAGE * D, PB = 2 * PE;  // elements and bytes of a page of one KV head
+  constexpr int LD = 8 / NC;                         // 1 KB loads per wavefront and step
+  static_assert(TRS % 2 == 0 && TRS <= 6 && 8 % NC == 0, "stages alternate between two score sets");
+  __shared__ __align__(1024) uint8_t s0[4 * PB];
+  __shared__ __align__(1024) uint8_t s1[4 * PB];
+  __shared__ __align__(1024) uint8_t s2[4 * PB];
+  __shared__ __align__(1024) uint8_t s3[4 * PB];
+  __shared__ __align__(1024) uint8_t s4[4 * PB];
+  __shared__ __align__(1024) uint8_t s5[4 * PB];
+  auto stage_of = [&](int s) __attribute__((always_inline)) {
+    return s == 0 ? s0 : s == 1 ? s1 : s == 2 ? s2 : s == 3 ? s3 : s == 4 ? s4 : s5;
+  };
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const unsigned hkv = P.hkv;
+  const int g = blockIdx.x % hkv, tile = blockIdx.x / hkv % (unsigned)tiles, item = blockIdx.x / hkv / (unsigned)tiles;
+  TreeItem it;
+  if (!load_item(P, item, it)) return;
+  const int G = P.hq / P.hkv, cols = it.n * G;
+  if (64 * NC * tile >= cols) return;
+  const int c0 = 64 * (NC * tile + wave);
+  const bool busy = c0 < cols;  // wave-uniform; a wavefront without columns only loads
+  const int32_t* ptab = P.page_table + (int64_t)it.b * P.max_pages;
+  const int n_steps = (it.pg1 - it.pg0 + 1) / 2;
+
+  // this lane's column in each of the wavefront's two tiles
+  const int fc = lane & 31, h = lane >> 5;
+  int node[2], head[2];
+  bool valid[2];
+  Sight sight[2];
+  Frag<bf16> qf[2][4];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int c = c0 + 32 * j + fc;
+    valid[j] = c < cols;
+    node[j] = min(c / G, it.n - 1);
+    head[j] = g * G + c % G;
+    sight[j] = sight_of(P, it, node[j]);
+    const bf16* qp = reinterpret_cast<const bf16*>(P.q) + ((int64_t)(it.t0 + node[j]) * P.hq + head[j]) * D + 8 * h;
+#pragma unroll
+    for (int cc = 0; cc < 4; ++cc) {
+      qf[j][cc].load(qp + 16 * cc);
+      qf[j][cc].keep_if(valid[j]);
+    }
+  }
+
+  // page ids of steps base .. base + 31, lane i: page pg0 + 2 base + i (the split's last page past its end). A
+  // block of IDB steps and the requests ahead of it find their ids in one register; the next block's are
+  // loaded a block ahead.
+  constexpr int IDB = 24;
+  static_assert(IDB % TRS == 0 && IDB + TRS - 1 <= 32, "a block's ids and those requested ahead of it");
+  auto ids_of = [&](int base) __attribute__((always_inline)) {
+    return ptab[min(it.pg0 + 2 * base + lane, it.pg1 - 1)];
+  };
+  int ids = ids_of(0), base = 0;
+  const int64_t page_bytes = (int64_t)P.hkv * PB;
+  // piece w of a step, 1 KB: half w % 2 of K of page 0, K of page 1, V of page 0, V of page 1 (w / 2). The 16-byte
+  // chunks of V are permuted on the way (128-byte block b of a 512-byte dim tile to b ^ (tile & 1)), so that the
+  // lanes of a half tile read all banks.
+  auto page_of = [&](int step, int which, bool& good) __attribute__((always_inline)) {
+    const int id = __builtin_amdgcn_readlane(ids, 2 * (step - base) + which);
+    good = id >= 0 && id < P.n_pages;
+    return good ? id : 0;
+  };
+  auto request = [&](uint8_t* stg, int step) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < LD; ++u) {
+      const int w = wave * LD + u;
+      bool good;
+      const int id = page_of(step, (w >> 1) & 1, good);
+      const uint8_t* pool = reinterpret_cast<const uint8_t*>(w < 4 ? P.k_pool : P.v_pool) + (int64_t)g * PB;
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<uint8_t*>(pool) + id * page_bytes, 0, PB, 0x00020000);
+      const uint32_t at = 1024u * (w & 1) + 16u * lane;
+      const uint32_t vo = w < 4 ? at : at ^ (((at >> 9) & 1u) << 7);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t)(stg + 1024 * w), 16, vo, 0, 0, 0);
+    }
+  };
+
+  constexpr float WEIGHT_LIMIT = 0x1p8f;       // of a lane's 16 weights in a step
+  float m_run[2], m_sub[2], limit[2], l[2];    // limit: -inf until a key is visible
+  f32x16 acc[2][2];                            // [dim tile][column tile]
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    m_run[j] = -INFINITY;
+    m_sub[j] = 0.f;
+    limit[j] = -INFINITY;
+    l[j] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[dt][j][e] = 0.f;
+  }
+  // fragment addresses: key fc of the step (page fc / 16), dims 8 h .. of a 16-dim chunk; dim fc of a tile of 32,
+  // value rows 4 h .. and 8 + 4 h ..
+  const uint32_t ko = (fc >> 4) * PB + ((h * 16 + (fc & 15)) * 16);
+  const uint32_t vbase = (fc >> 4) * 512 + (fc & 15) * 8 + (((uint32_t)h ^ ((fc >> 4) & 1)) << 7);
+
+  struct Scores {
+    f32x16 t[2];
+  };
+  auto load_keys = [&](u32x4_t (&kf)[4], const uint8_t* stg) __attribute__((always_inline)) {
+#pragma unroll
+    for (int cc = 0; cc < 4; ++cc) kf[cc] = *reinterpret_cast<const u32x4_t*>(stg + ko + 512 * cc);
+  };
+  auto scores = [&](Scores& sc, const u32x4_t (&kf)[4]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc.t[j][e] = 0.f;
+#pragma unroll
+    for (int cc = 0; cc < 4; ++cc)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        sc.t[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[cc]),
+                                                          __builtin_bit_cast(bf16x8_t, qf[j][cc].v), sc.t[j], 0, 0, 0);
+  };
+  // the keys of a step that a column sees, bit i: key i
+  auto visible = [&](int j, int k0, uint32_t pages) __attribute__((always_inline)) {
+    const int off = k0 - it.len, lo = sight[j].lo - k0;  // first node, first committed key in sight
+    const uint64_t nodes = off >= 0 ? (off < 64 ? sight[j].seen >> off : 0) : (off > -32 ? sight[j].seen << -off : 0);
+    const uint32_t old = off >= 0 ? 0u : off > -32 ? (1u << -off) - 1u : ~0u;
+    const uint32_t left = lo <= 0 ? 0u : lo < 32 ? (1u << lo) - 1u : ~0u;
+    return valid[j] ? ((uint32_t)nodes | (old & ~left)) & pages : ~0u;
+  };
+  // a step's softmax and value products from its scores, and the scores of the next step
+  auto attend = [&](Scores& sc, Scores& sn, const uint8_t* stg, const uint8_t* nxt, int step) __attribute__((always_inline)) {
+    u32x4_t kf[4];
+    load_keys(kf, nxt);
+    bool ok[2];
+    page_of(step, 0, ok[0]);
+    page_of(step, 1, ok[1]);
+    const int pg = it.pg0 + 2 * step, k0 = pg * PAGE;
+    const bool second = pg + 1 < it.pg1;
+    const bool edge = k0 + 2 * PAGE > it.len || (P.window > 0 && k0 < it.len + it.n - P.window) || !ok[0] || !ok[1] || !second;
+    uint32_t vis[2];
+    if (__builtin_expect(edge, 0)) {  // wave-uniform; the empty asm keeps it a branch
+      asm volatile("");
+      if ((!ok[0] || (!ok[1] && second)) && lane == 0) set_error(P.err, 1);
+      const uint32_t pages = (ok[0] ? 0xFFFFu : 0u) | (ok[1] && second ? 0xFFFF0000u : 0u);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        vis[j] = visible(j, k0, pages);
+        const uint32_t mine = vis[j] >> (4 * h);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc.t[j][e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? sc.t[j][e] : -INFINITY;
+      }
+    }
+    u32x4_t pw[2][2];  // [column tile][page]: the weights, packed
+    float sum[2];
+    auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        sum[j] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(sc.t[j][e], P.scale_log2, -m_sub[j]));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(sc.t[j][e + 1], P.scale_log2, -m_sub[j]));
+          const uint32_t w = pack_bf16(p0, p1);
+          pw[j][e >> 3][(e & 7) >> 1] = w;
+          sum[j] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w), __builtin_bit_cast(bf16x2_t, 0x3F803F80u), sum[j], false);
+        }
+      }
+    };
+    __builtin_amdgcn_sched_barrier(0);
+    scores(sn, kf);
+    weights();
+    // the next scores' eight products among the 96 vector instructions of the weights
+#define TREE_MIX                                      \
+  __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  \
+  __builtin_amdgcn_sched_group_barrier(0x402, 12, 0);
+    TREE_MIX TREE_MIX TREE_MIX TREE_MIX TREE_MIX TREE_MIX TREE_MIX TREE_MIX
+#undef TREE_MIX
+    // The maximum only has to keep the weights in range, so it is raised when a step's sum says that they are
+    // not, and until a column has seen a key; the weights are then formed again.
+    const bool raise = sum[0] > limit[0] || sum[1] > limit[1];
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(raise) != 0, 0)) {  // wave-uniform (kept a branch)
+      asm volatile("");
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float mloc = sc.t[j][0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) mloc = vmax(mloc, sc.t[j][e]);
+        const uint32_t u = __float_as_uint(mloc);
+        auto sw = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        const float mstep = vmax(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * P.scale_log2;
+        // a column's own lanes decide, so that its bits do not depend on the columns beside it
+        const uint32_t o = sum[j] > limit[j];
+        auto so = __builtin_amdgcn_permlane32_swap(o, o, false, false);
+        const float m_new = (so[0] | so[1]) ? fmaxf(m_run[j], mstep) : m_run[j];
+        const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[j] - m_new);
+        l[j] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt) acc[dt][j] *= alpha;
+        m_run[j] = m_new;
+        m_sub[j] = m_new == -INFINITY ? 0.f : m_new;  // masked scores give 2^-inf = 0
+        limit[j] = m_new == -INFINITY ? -INFINITY : WEIGHT_LIMIT;
+      }
+      weights();
+    }
+    u32x4_t vf[2][2];  // [page][dim tile]
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int dt = 0; dt < 2; ++dt) {
+        const uint8_t* v = stg + (2 + p) * PB + 1024 * dt + vbase;
+        const u32x2_t a = *reinterpret_cast<const u32x2_t*>(v), c = *reinterpret_cast<const u32x2_t*>(v + 256);
+        vf[p][dt] = __builtin_shufflevector(a, c, 0, 1, 2, 3);
+      }
+    if (__builtin_expect(edge, 0)) {
+      asm volatile("");
+      bool odd = false;
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t w = vf[p][dt][i];
+            odd |= drop_nonfinite(w);
+            vf[p][dt][i] = w;
+          }
+      if (__builtin_amdgcn_ballot_w64(odd) != 0) {  // rare: values that are not finite, for the columns that see them
+        for (int key = 0; key < 2 * PAGE; ++key) {
+          const uint8_t* page = stg + (2 + (key >> 4)) * PB;
+          const int slot = key & 15;
+#pragma unroll
+          for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int dim = 32 * dt + 8 * (e >> 2) + 4 * h + (e & 3);
+              const uint32_t at = 2 * v_off(slot, dim);
+              const uint16_t bits = *reinterpret_cast<const uint16_t*>(page + (at ^ (((at >> 9) & 1u) << 7)));
+              const bool bad = (bits & 0x7F80u) == 0x7F80u;
+#pragma unroll
+              for (int j = 0; j < 2; ++j)
+                acc[dt][j][e] += bad && (vis[j] >> key & 1) ? bf16_to_f32(bits) : 0.f;
+            }
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      l[j] += sum[j];
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt)
+          acc[dt][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf[p][dt]),
+                                                               __builtin_bit_cast(bf16x8_t, pw[j][p]), acc[dt][j], 0, 0, 0);
+    }
+  };
+
+  // Step s sits in stage s % TRS. In step s its scores are there already; step s + TRS - 1 is requested into the
+  // stage step s - 1 left, the scores of step s + 1 are formed, and before the barrier a wavefront waits for its
+  // loads of step s + 2. The barrier hands the stages over: this wavefront's reads of the step's stage have
+  // returned (lgkmcnt), its loads of step s + 2 have landed, and the empty asm keeps LDS accesses on their side.
+  auto publish = [&]() __attribute__((always_inline)) {
+    constexpr int N = LD * (TRS - 3);  // loads that may stay in flight
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (N >> 4 << 14));  // vmcnt(N) expcnt(7) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+#pragma unroll
+  for (int s = 0; s < TRS - 1; ++s) {
+    request(stage_of(s), s);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  publish();
+  Scores sc[2];
+  if (busy) {
+    u32x4_t kf[4];
+    load_keys(kf, s0);
+    scores(sc[0], kf);
+  }
+  auto one = [&](auto U_, int step) __attribute__((always_inline)) {
+    constexpr int U = decltype(U_)::value;
+    if (step < n_steps) {  // uniform
+      request(stage_of((U + TRS - 1) % TRS), step + TRS - 1);
+      if (busy) attend(sc[U % 2], sc[(U + 1) % 2], stage_of(U), stage_of((U + 1) % TRS), step);
+    }
+    publish();
+  };
+  while (true) {
+    const int ids_next = ids_of(base + IDB), stop = min(n_steps, base + IDB);
+    for (int step = base; step < stop; step += TRS) {
+      one(std::integral_constant<int, 0>{}, step);
+      one(std::integral_constant<int, 1>{}, step + 1);
+      one(std::integral_constant<int, 2>{}, step + 2);
+      one(std::integral_constant<int, 3>{}, step + 3);
+      if constexpr (TRS > 4) {
+        one(std::integral_constant<int, 4>{}, step + 4);
+        one(std::integral_constant<int, 5>{}, step + 5);
+      }
+    }
+    if (stop == n_steps) break;
+    base = stop;
+    ids = ids_next;
+  }
+  __builtin_amdgcn_s_waitcnt(0);  // no load into LDS may outlive the workgroup
+
+  // this lane's dims 32 dt + 8 q + 4 h .. + 3 of each column: a partial row, or o with the sink
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const uint32_t u = __float_as_uint(l[j]);
+    auto sw = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    float l_tot = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    if (!valid[j]) continue;
+    if (it.splits > 1) {
+      const int64_t row = (int64_t)(it.row0 + node[j]) * P.hq + head[j];
+      if (h == 0) *reinterpret_cast<float2*>(P.part_ml + 2 * row) = make_float2(m_run[j], l_tot);
+#pragma unroll
+      for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<float4*>(P.part_acc + row * D + 32 * dt + 8 * q + 4 * h) =
+              make_float4(acc[dt][j][4 * q], acc[dt][j][4 * q + 1], acc[dt][j][4 * q + 2], acc[dt][j][4 * q + 3]);
+      continue;
+    }
+    float f = 1.0f;
+    if (P.sinks) {
+      const float sk = P.sinks[head[j]] * LOG2E, M = fmaxf(m_run[j], sk);
+      f = m_run[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[j] - M);
+      l_tot = l_tot * f + __builtin_amdgcn_exp2f(sk - M);
+    }
+    const float inv = l_tot == 0.f ? 0.f : f / l_tot;
+    bf16* o = reinterpret_cast<bf16*>(P.o) + ((int64_t)(it.t0 + node[j]) * P.hq + head[j]) * D + 4 * h;
+#pragma unroll
+    for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        store4(o + 32 * dt + 8 * q, make_float4(acc[dt][j][4 * q] * inv, acc[dt][j][4 * q + 1] * inv,
+                                                acc[dt][j][4 * q + 2] * inv, acc[dt][j][4 * q + 3] * inv));
+  }
+}
+
+template <int NC, int TRS>
+static hipError_t tree_wide_impl(const TreeAttn& p, hipStream_t s) {
+  const int cols = p.max_nodes * (p.hq / p.hkv), tiles = (cols + 64 * NC - 1) / (64 * NC);
+  const int64_t blocks = (int64_t)p.n_items * p.hkv * tiles;
+  if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((tree_attn_wide_kernel<NC, TRS>), dim3((unsigned)blocks), dim3(64 * NC), 0, s, p, tiles);
+  return hipGetLastError();
+}
+
 hipError_t launch_tree_attn(int dtype, int head_dim, const TreeAttn& p, hipStream_t s) {
   if (p.n_items == 0) return hipSuccess;
+  // bf16 with head dim 64 takes the wide products, whose pages go to LDS by 16-byte direct loads: 16-byte
+  // aligned pools only. As many wavefronts as the largest tree has columns share a page.
+  if (dtype == 1 && head_dim == 64 && ((uintptr_t)p.k_pool | (uintptr_t)p.v_pool) % 16 == 0) {
+    const int cols = p.max_nodes * (p.hq / p.hkv);
+    if (cols <= 64) return tree_wide_impl<1, 4>(p, s);
+    if (cols <= 128) return tree_wide_impl<2, 6>(p, s);
+    if (cols <= 256) return tree_wide_impl<4, 6>(p, s);
+    return tree_wide_impl<8, 6>(p, s);
+  }
   if (dtype == 0) return head_dim == 32 ? tree_attn_impl<float, 32>(p, s) : tree_attn_impl<float, 64>(p, s);
   return head_dim == 32 ? tree_attn_impl<bf16, 32>(p, s) : tree_attn_impl<bf16, 64>(p, s);
 }
