@@ -8,61 +8,59 @@ namespace mcpu {
 
 constexpr int TREE_MAX_NODES = 64;  // a node's ancestors are the bits of one 64-bit word
 
-// Node i of its tree: bit a of `seen` is set if node a is an ancestor of i (or
-// i itself) inside i's window; depth = ancestors without i.
-struct TreeNode {
-  uint64_t seen;
-  int32_t depth, pad;
-};
-
 // One split of a tree's visible pages: n nodes (rows t0 ..) of sequence b behind
 // len committed tokens, logical pages pg0 .. pg1 - 1. Its partial rows (node i of
-// part_ml / part_acc at row0 + i) exist where the tree has more than one split
-// (splits > 1); a tree's only split writes o itself.
+// part_ml / part_acc at row0 + i) exist where the tree has more than one split; a
+// tree's only split writes o itself.
 struct TreeItem {
   int32_t b, t0, n, len, pg0, pg1, row0, splits;
 };
+constexpr int TREE_SCAN = 256;  // up to this many sequences the items are found without a plan launch
 
-struct TreePlan {
+struct TreeArgs {
   const int32_t* seq_lens;  // [batch]
   const int32_t* cu_q;      // [batch + 1]
   const int32_t* parents;   // [n_tokens]
-  int batch, n_tokens, max_pages, window, pps;
-  int n_items, n_rows;      // what the host planned; checked on the device
-  TreeNode* node;           // [n_tokens] out
-  TreeItem* item;           // [n_items] out
-  int32_t* tok_seq;         // [n_tokens] out
-  int2* seq_split;          // [batch] out: first partial row, number of splits
+  int batch, n_tokens, max_pages, window;
+  int pps;                  // pages per split
+  int n_items, n_rows;      // splits and partial rows as the host counted them, checked on the device; without
+                            // partial rows item i is tree i (n_items = batch)
+  const TreeItem* item;     // [n_items] from the plan kernel, or nullptr
   int32_t* err;
 };
-hipError_t launch_tree_plan(const TreePlan& p, hipStream_t s);
+hipError_t launch_tree_plan(const TreeArgs& p, TreeItem* out, hipStream_t s);
 
-struct TreeAttn {
+// How a step's columns (node and query head pairs of one KV head) are dealt out:
+// `cols` of them to each workgroup (each wavefront for TREE_ANY), of which `per_cu`
+// are at work on a compute unit at a time.
+enum TreeKind { TREE_ANY, TREE_NARROW1, TREE_NARROW2, TREE_WIDE1, TREE_WIDE2, TREE_WIDE4 };
+struct TreeForm {
+  int kind, cols, per_cu;
+};
+TreeForm tree_attn_form(int dtype, int head_dim, const void* k_pool, const void* v_pool, int cols, bool light);
+
+struct TreeAttn : TreeArgs {
   const void* q;  // [n_tokens][Hq][D]
   const void* k_pool;
   const void* v_pool;
   const int32_t* page_table;
-  int max_pages, n_pages;
-  const TreeNode* node;
-  const TreeItem* item;
-  int batch, n_tokens, n_items, n_rows, max_nodes, hq, hkv, window;
+  int n_pages, max_nodes, hq, hkv;
+  TreeForm form;
   float scale_log2;    // log2(e) / sqrt(D)
   const float* sinks;  // [Hq] or nullptr
   float* part_ml;      // [n_rows][Hq][2] running max (log2 units) and sum
   float* part_acc;     // [n_rows][Hq][D]
+  int4* tok;           // [n_tokens] out where n_rows > 0: first partial row, rows per split, splits
   void* o;             // [n_tokens][Hq * D]
-  int32_t* err;
 };
 hipError_t launch_tree_attn(int dtype, int head_dim, const TreeAttn& p, hipStream_t s);
 
 struct TreeCombine {
   const float* part_ml;
   const float* part_acc;
-  const int32_t* cu_q;
-  const int32_t* tok_seq;
-  const int2* seq_split;
+  const int4* tok;
   const float* sinks;
-  int batch, n_tokens, n_rows, hq;
+  int n_tokens, n_rows, hq;
   void* o;
 };
 hipError_t launch_tree_combine(int dtype, int head_dim, const TreeCombine& p, hipStream_t s);

@@ -453,71 +453,101 @@ int collect_pools(mcpu_kv_pool* const* pools, int32_t n_pools, PoolSet* out, int
 
 // ---- trees of drafted tokens -------------------------------------------------
 
+constexpr int N_CU = 256;
 constexpr int TREE_EXTRA_ROWS = 4096;  // partial rows beyond one per node that the workspace holds
+constexpr int TREE_PPS_MIN = 12;       // pages per split at least (measured: 8 to 16 are within a microsecond)
+constexpr int TREE_START_PAGES = 32;   // what starting and ending a split costs, in pages
 
 struct TreePlanHost {
   int n_tokens = 0, max_nodes = 0, max_pos = 0;
-  int pps = 0, n_items = 0, n_rows = 0;
+  int pps = 1, n_items = 0, n_rows = 0;
+  TreeForm form{};
 };
 
 // Validate host positions and choose the pages per split, so that the splits
 // fill the GPU and their partial rows fit the workspace.
-int plan_tree(const mcpu_layer_cfg* c, int batch, int max_pages, const int32_t* hsl, const int32_t* hcu,
-              TreePlanHost* out) {
+int plan_tree(const mcpu_layer_cfg* c, const mcpu_kv_pool* pool, int batch, int max_pages, const int32_t* hsl,
+              const int32_t* hcu, TreePlanHost* out) {
   if (!hsl || !hcu) return fail(MCPU_EINVAL, "host_seq_lens or host_cu_q is NULL");
   if (hcu[0] != 0) return fail(MCPU_EINVAL, "host_cu_q[0] must be 0");
   auto pages_of = [&](int b, int n) {
     const int lo = c->window > 0 ? std::max(0, hsl[b] - c->window + 1) : 0;
-    return (hsl[b] + n - 1) / PAGE_SIZE - lo / PAGE_SIZE + 1;
+    return n > 0 ? (hsl[b] + n - 1) / PAGE_SIZE - lo / PAGE_SIZE + 1 : 0;
   };
   long long total = 0;
+  int longest = 0;
   for (int b = 0; b < batch; ++b) {
     const int n = hcu[b + 1] - hcu[b];
     if (n < 0) return fail(MCPU_EINVAL, "host_cu_q is not non-decreasing at %d", b);
     if (n > TREE_MAX_NODES) return fail(MCPU_EUNSUPPORTED, "tree %d has %d nodes (at most %d)", b, n, TREE_MAX_NODES);
     if (hsl[b] < 0) return fail(MCPU_EINVAL, "seq_lens[%d] = %d < 0", b, hsl[b]);
-    if (n == 0) continue;
-    if (((long long)hsl[b] + n - 1) / PAGE_SIZE >= max_pages)
+    if (n > 0 && ((long long)hsl[b] + n - 1) / PAGE_SIZE >= max_pages)
       return fail(MCPU_EINVAL, "sequence %d position %lld beyond page table width %d", b, (long long)hsl[b] + n - 1, max_pages);
     out->max_nodes = std::max(out->max_nodes, n);
-    out->max_pos = std::max(out->max_pos, hsl[b] + n - 1);
+    if (n > 0) out->max_pos = std::max(out->max_pos, hsl[b] + n - 1);
+    longest = std::max(longest, pages_of(b, n));
     total += pages_of(b, n);
   }
   out->n_tokens = hcu[batch];
-  const long long target = std::max<long long>(1, (long long)TARGET_WAVES / c->n_kv_heads);
-  long long pps = std::max<long long>(PPS_MIN, (total + target - 1) / target);
-  for (;; pps *= 2) {
-    long long items = 0, rows = 0;
-    for (int b = 0; b < batch; ++b) {
-      const int n = hcu[b + 1] - hcu[b];
-      if (n == 0) continue;
-      const long long splits = (pages_of(b, n) + pps - 1) / pps;
-      items += splits;
-      if (splits > 1) rows += splits * n;
-    }
-    if (rows > (long long)out->n_tokens + TREE_EXTRA_ROWS) continue;  // ends: one split each leaves no row
-    out->pps = (int)std::min<long long>(pps, INT32_MAX);
-    out->n_items = (int)items;
-    out->n_rows = (int)rows;
+  const int cols = out->max_nodes * (c->n_q_heads / c->n_kv_heads);
+  const bool one_each = longest <= 2 * TREE_PPS_MIN;
+  out->form = tree_attn_form(c->dtype, c->head_dim, pool->k, pool->v, cols,
+                             one_each || total * c->n_kv_heads <= 4 * N_CU * TREE_PPS_MIN);
+  if (one_each) {  // short trees: no tree is split
+    out->pps = 2 * TREE_PPS_MIN;
+    out->n_items = batch;
     return MCPU_OK;
   }
+  // splits of a given length, and their partial rows
+  auto count = [&](long long pps, long long* rows) {
+    long long items = 0;
+    *rows = 0;
+    for (int b = 0; b < batch; ++b) {
+      const int n = hcu[b + 1] - hcu[b], splits = (int)((pages_of(b, n) + pps - 1) / pps);
+      items += splits;
+      if (splits > 1) *rows += (long long)splits * n;
+    }
+    return items;
+  };
+  // one or two rounds of workgroups, as their length and start cost come out shorter; the second round of a
+  // large batch evens out its short trees
+  const int tiles = (cols + out->form.cols - 1) / out->form.cols;
+  const long long slots = std::max(1, N_CU * out->form.per_cu / (c->n_kv_heads * tiles));
+  long long best = -1, pps = TREE_PPS_MIN, rows = 0;
+  for (int r = batch > 64 ? 2 : 1; r <= 2; ++r) {
+    long long p = std::max<long long>(TREE_PPS_MIN, (total + slots * r - 1) / (slots * r)), items = 0;
+    for (int k = 0; k < 6; ++k, p += p / 12 + 1) {  // trees do not divide evenly: longer until the round holds them
+      items = count(p, &rows);
+      if (items <= slots * r || items <= batch) break;
+    }
+    const long long cost = (items + slots - 1) / slots * (p + TREE_START_PAGES);
+    if (best < 0 || cost < best) {
+      best = cost;
+      pps = p;
+    }
+  }
+  long long items = count(pps, &rows);
+  while (rows > (long long)out->n_tokens + TREE_EXTRA_ROWS) {  // ends: trees with one split have no rows
+    pps += pps / 8 + 1;
+    items = count(pps, &rows);
+  }
+  out->pps = (int)pps;
+  out->n_items = rows == 0 ? batch : (int)items;
+  out->n_rows = (int)rows;
+  return MCPU_OK;
 }
 
 struct TreeBufs {
-  TreeNode* node;
   TreeItem* item;
-  int32_t* tok_seq;
-  int2* seq_split;
+  int4* tok;
   float *part_ml, *part_acc;
 };
 
 TreeBufs carve_tree(Carve& cv, const mcpu_layer_cfg* c, int max_batch, int max_tokens) {
   TreeBufs b;
   const size_t rows = (size_t)max_tokens + TREE_EXTRA_ROWS;
-  b.node = cv.take<TreeNode>(max_tokens);
   b.item = cv.take<TreeItem>(rows + max_batch);  // a split has a row at least, a tree without splits is one item
-  b.tok_seq = cv.take<int32_t>(max_tokens);
-  b.seq_split = cv.take<int2>(max_batch);
+  b.tok = cv.take<int4>(max_tokens);
   b.part_ml = cv.take<float>(rows * c->n_q_heads * 2);
   b.part_acc = cv.take<float>(rows * c->n_q_heads * c->head_dim);
   return b;
@@ -527,30 +557,28 @@ int run_tree_attention(const mcpu_layer_cfg* c, const float* sinks, mcpu_kv_pool
                        const int32_t* page_table, int max_pages, const int32_t* seq_lens, const int32_t* cu_q,
                        const int32_t* parents, const TreePlanHost& ph, const void* q, void* o, const TreeBufs& tb,
                        int32_t* err, hipStream_t st) {
-  TreePlan pl{};
-  pl.seq_lens = seq_lens; pl.cu_q = cu_q; pl.parents = parents; pl.batch = batch; pl.n_tokens = ph.n_tokens;
-  pl.max_pages = max_pages; pl.window = c->window; pl.pps = ph.pps; pl.n_items = ph.n_items; pl.n_rows = ph.n_rows;
-  pl.node = tb.node; pl.item = tb.item; pl.tok_seq = tb.tok_seq; pl.seq_split = tb.seq_split; pl.err = err;
-  {
-    Timed tm(MCPU_KERNEL_TREE_PLAN, st);
-    HIP_TRY(launch_tree_plan(pl, st));
-  }
   TreeAttn ta{};
-  ta.q = q; ta.k_pool = pool->k; ta.v_pool = pool->v; ta.page_table = page_table; ta.max_pages = max_pages;
-  ta.n_pages = pool->n_pages; ta.node = tb.node; ta.item = tb.item; ta.batch = batch; ta.n_tokens = ph.n_tokens;
-  ta.n_items = ph.n_items; ta.n_rows = ph.n_rows; ta.max_nodes = ph.max_nodes; ta.hq = c->n_q_heads;
-  ta.hkv = c->n_kv_heads; ta.window = c->window;
+  ta.seq_lens = seq_lens; ta.cu_q = cu_q; ta.parents = parents; ta.batch = batch; ta.n_tokens = ph.n_tokens;
+  ta.max_pages = max_pages; ta.window = c->window; ta.pps = ph.pps; ta.n_items = ph.n_items; ta.n_rows = ph.n_rows;
+  ta.err = err;
+  if (batch > TREE_SCAN && ph.n_rows > 0) {
+    Timed tm(MCPU_KERNEL_TREE_PLAN, st);
+    HIP_TRY(launch_tree_plan(ta, tb.item, st));
+    ta.item = tb.item;
+  }
+  ta.q = q; ta.k_pool = pool->k; ta.v_pool = pool->v; ta.page_table = page_table; ta.n_pages = pool->n_pages;
+  ta.form = ph.form;
+  ta.max_nodes = ph.max_nodes; ta.hq = c->n_q_heads; ta.hkv = c->n_kv_heads;
   ta.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c->head_dim));
-  ta.sinks = sinks; ta.part_ml = tb.part_ml; ta.part_acc = tb.part_acc; ta.o = o; ta.err = err;
+  ta.sinks = sinks; ta.part_ml = tb.part_ml; ta.part_acc = tb.part_acc; ta.tok = tb.tok; ta.o = o;
   {
     Timed tm(MCPU_KERNEL_TREE_ATTN, st);
     HIP_TRY(launch_tree_attn(c->dtype, c->head_dim, ta, st));
   }
   if (ph.n_rows == 0) return MCPU_OK;
   TreeCombine cb{};
-  cb.part_ml = tb.part_ml; cb.part_acc = tb.part_acc; cb.cu_q = cu_q; cb.tok_seq = tb.tok_seq;
-  cb.seq_split = tb.seq_split; cb.sinks = sinks; cb.batch = batch; cb.n_tokens = ph.n_tokens; cb.n_rows = ph.n_rows;
-  cb.hq = c->n_q_heads; cb.o = o;
+  cb.part_ml = tb.part_ml; cb.part_acc = tb.part_acc; cb.tok = tb.tok; cb.sinks = sinks; cb.n_tokens = ph.n_tokens;
+  cb.n_rows = ph.n_rows; cb.hq = c->n_q_heads; cb.o = o;
   Timed tm(MCPU_KERNEL_TREE_COMBINE, st);
   HIP_TRY(launch_tree_combine(c->dtype, c->head_dim, cb, st));
   return MCPU_OK;
@@ -730,7 +758,7 @@ int tree_attention(const mcpu_layer_cfg* cfg, const float* sinks, mcpu_kv_pool* 
   if (batch <= 0 || max_pages <= 0) return fail(MCPU_EINVAL, "batch %d, max_pages %d", batch, max_pages);
   if (!page_table || !seq_lens || !cu_q || !workspace) return fail(MCPU_EINVAL, "NULL pointer");
   TreePlanHost ph;
-  if ((rc = plan_tree(cfg, batch, max_pages, host_seq_lens, host_cu_q, &ph))) return rc;
+  if ((rc = plan_tree(cfg, pool, batch, max_pages, host_seq_lens, host_cu_q, &ph))) return rc;
   if (ph.n_tokens == 0) return MCPU_OK;
   if (!parents || !q || !o) return fail(MCPU_EINVAL, "NULL pointer");
   if ((uintptr_t)q % 16 || (uintptr_t)o % 16) return fail(MCPU_EINVAL, "q and o must be 16-byte aligned");

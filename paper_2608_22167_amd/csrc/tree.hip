@@ -19,139 +19,197 @@ namespace mcpu {
 constexpr float LOG2E = 1.4426950408889634f;
 
 // ---------------------------------------------------------------------------
-// plan
+// plan: which pages of which tree a workgroup attends to
 // ---------------------------------------------------------------------------
 
 __device__ __forceinline__ int first_page(int len, int window) {
   return (window > 0 ? max(0, len - window + 1) : 0) / PAGE;
 }
 
-// Ancestor masks and depths of one tree by one wavefront, lane i = node i, by
-// pointer doubling: after round r lane i has the union of its first 2^r ancestors
-// and points 2^r steps up. A parent outside [-1, i) raises bit 64 and counts as -1.
-__device__ void tree_nodes(const TreePlan& P, int b) {
-  const int lane = lane_id();
-  const int t0 = P.cu_q[b], n = P.cu_q[b + 1] - t0;
-  if (n <= 0 || n > TREE_MAX_NODES || t0 < 0 || t0 + n > P.n_tokens) return;  // raised by the split part
-  int up = lane < n ? P.parents[t0 + lane] : -1;
-  if (up < -1 || up >= lane) {
-    if (lane < n) set_error(P.err, 64);
-    up = -1;
-  }
-  const int parent = up;
-  uint64_t seen = 1ull << lane;
-#pragma unroll
-  for (int r = 0; r < 6; ++r) {
-    const int from = max(up, 0);
-    const uint32_t lo = __shfl((uint32_t)seen, from, 64), hi = __shfl((uint32_t)(seen >> 32), from, 64);
-    const int next = __shfl(up, from, 64);
-    if (up >= 0) {
-      seen |= (uint64_t)hi << 32 | lo;
-      up = next;
-    }
-  }
-  const int depth = __popcll(seen) - 1;
-  // a window shorter than the branch drops the ancestors that lie window or more steps up
-  if (P.window > 0 && __ballot(depth >= P.window) != 0) {
-    uint64_t near = 1ull << lane;
-    int a = parent;
-    for (int k = 1; k < TREE_MAX_NODES; ++k) {
-      if (a >= 0 && k < P.window) near |= 1ull << a;
-      const int next = __shfl(parent, max(a, 0), 64);
-      a = a >= 0 ? next : -1;
-    }
-    seen = near;
-  }
-  if (lane < n) {
-    TreeNode d;
-    d.seen = seen;
-    d.depth = depth;
-    d.pad = 0;
-    P.node[t0 + lane] = d;
-    P.tok_seq[t0 + lane] = b;
-  }
+// Sequence b's tree, its pages and its splits; none for an empty tree, for b past
+// the batch and for device arrays that do not fit the call, which raise bit 8 if
+// `report`.
+struct TreeSpan {
+  int t0, n, len, pages, splits;
+};
+__device__ __forceinline__ TreeSpan tree_span(const TreeArgs& P, int b, bool report) {
+  const int at = min(b, P.batch - 1);  // loads without a branch, so that several spans' are in flight together
+  TreeSpan s;
+  s.t0 = P.cu_q[at];
+  s.n = P.cu_q[at + 1] - s.t0;
+  s.len = P.seq_lens[at];
+  const bool bad = s.n < 0 || s.n > TREE_MAX_NODES || s.t0 < 0 || s.t0 > P.n_tokens - s.n || s.len < 0 ||
+                   (s.n > 0 && (s.len > INT32_MAX - TREE_MAX_NODES || (s.len + s.n - 1) / PAGE >= P.max_pages));
+  if (bad && report) set_error(P.err, 8);
+  s.n = bad || b >= P.batch ? 0 : s.n;
+  s.pages = s.n > 0 ? (s.len + s.n - 1) / PAGE - first_page(s.len, P.window) + 1 : 0;
+  s.splits = (s.pages + P.pps - 1) / P.pps;
+  return s;
+}
+// partial rows of a tree: its nodes once per split, if there are several
+__device__ __forceinline__ int rows_of(const TreeSpan& s) { return s.splits > 1 ? s.splits * s.n : 0; }
+
+// Split k of a tree, whose pages the splits share evenly.
+__device__ __forceinline__ TreeItem split_of(const TreeArgs& P, const TreeSpan& s, int b, int row0, int k) {
+  const int first = first_page(s.len, P.window);
+  TreeItem it;
+  it.b = b; it.t0 = s.t0; it.n = s.n; it.len = s.len; it.splits = s.splits;
+  it.pg0 = first + (int)((int64_t)k * s.pages / s.splits);
+  it.pg1 = first + (int)((int64_t)(k + 1) * s.pages / s.splits);
+  it.row0 = row0 + k * s.n;
+  return it;
 }
 
-// Exclusive prefix of `local` over the block's threads, and the total.
-__device__ int plan_scan(int local, int* sums, int& total) {
-  const int incl = wave_incl_scan(local), wave = threadIdx.x >> 6, lane = lane_id(), nw = blockDim.x >> 6;
-  __syncthreads();  // sums may still be read for the scan before
-  if (lane == 63) sums[wave] = incl;
-  __syncthreads();
-  int before = 0;
-  total = 0;
-  for (int w = 0; w < nw; ++w) {
-    before += w < wave ? sums[w] : 0;
-    total += sums[w];
-  }
-  return before + incl - local;
-}
-
-// Workgroup 0: the splits, a thread per sequence. Workgroups 1..: the nodes, a
-// wavefront per sequence. Bound by latency.
-__global__ __launch_bounds__(1024) void tree_plan_kernel(TreePlan P) {
-  if (blockIdx.x > 0) {
-    const int b = (blockIdx.x - 1) * 16 + uniform(threadIdx.x >> 6);
-    if (b < P.batch) tree_nodes(P, b);
-    return;
-  }
-  __shared__ int sums[16];
+// The plan of a large batch, by one workgroup: a thread per sequence, and the
+// records of a wavefront's 64 trees written together, lane j the j-th.
+__global__ __launch_bounds__(1024) void tree_plan_kernel(TreeArgs P, TreeItem* out) {
+  __shared__ int sums[2][16];
+  const int lane = lane_id(), wave = threadIdx.x >> 6;
   int items = 0, rows = 0;
-  for (int base = 0; base < P.batch; base += blockDim.x) {
+  for (int base = 0; base < P.batch; base += 1024) {
     const int b = base + threadIdx.x;
-    TreeItem it{};
-    int np = 0;
-    if (b < P.batch) {
-      it.b = b;
-      it.t0 = P.cu_q[b];
-      it.n = P.cu_q[b + 1] - it.t0;
-      it.len = P.seq_lens[b];
-      if (it.n < 0 || it.n > TREE_MAX_NODES || it.t0 < 0 || it.t0 + it.n > P.n_tokens || it.len < 0 ||
-          (it.n > 0 && (it.len + it.n - 1) / PAGE >= P.max_pages)) {
-        set_error(P.err, 8);
-        it.n = 0;
-      }
-      if (it.n > 0) {
-        np = (it.len + it.n - 1) / PAGE - first_page(it.len, P.window) + 1;
-        it.splits = (np + P.pps - 1) / P.pps;
-      }
+    const TreeSpan s = tree_span(P, b, true);
+    const int incl = wave_incl_scan(s.splits), rincl = wave_incl_scan(rows_of(s));
+    __syncthreads();  // sums may still be read for the tile before
+    if (lane == 63) {
+      sums[0][wave] = incl;
+      sums[1][wave] = rincl;
     }
-    int all_items, all_rows;
-    const int at = items + plan_scan(it.splits, sums, all_items);
-    it.row0 = rows + plan_scan(it.splits > 1 ? it.splits * it.n : 0, sums, all_rows);
-    items += all_items;
-    rows += all_rows;
-    if (b < P.batch) {
-      P.seq_split[b] = make_int2(it.row0, it.splits);
-      const int first = first_page(it.len, P.window), n_splits = it.splits;
-      const int row0 = it.row0;
-      for (int k = 0; k < n_splits && at + k < P.n_items; ++k) {  // the pages shared out evenly
-        it.pg0 = first + (int)((int64_t)k * np / n_splits);
-        it.pg1 = first + (int)((int64_t)(k + 1) * np / n_splits);
-        it.row0 = row0 + k * it.n;
-        P.item[at + k] = it;
-      }
+    __syncthreads();
+    int at = items, row0 = rows + rincl - rows_of(s);
+    for (int w = 0; w < 16; ++w) {
+      at += w < wave ? sums[0][w] : 0;
+      row0 += w < wave ? sums[1][w] : 0;
+      items += sums[0][w];
+      rows += sums[1][w];
+    }
+    const int all = __shfl(incl, 63, 64);
+    for (int j0 = 0; j0 < all; j0 += 64) {
+      const int j = j0 + lane;
+      int o = 0;  // the first lane with incl > j: the tree of record j
+#pragma unroll
+      for (int step = 32; step; step >>= 1) o += __shfl(incl, o + step - 1, 64) <= j ? step : 0;
+      const int src = min(o, 63);
+      TreeSpan r;
+      r.t0 = __shfl(s.t0, src, 64); r.n = __shfl(s.n, src, 64); r.len = __shfl(s.len, src, 64);
+      r.pages = __shfl(s.pages, src, 64); r.splits = __shfl(s.splits, src, 64);
+      const int k = j - (__shfl(incl, src, 64) - r.splits), rb = __shfl(b, src, 64), rr = __shfl(row0, src, 64);
+      if (j < all && at + j < P.n_items) out[at + j] = split_of(P, r, rb, rr, k);
     }
   }
   if (threadIdx.x == 0 && (items != P.n_items || rows != P.n_rows)) set_error(P.err, 8);
 }
 
-hipError_t launch_tree_plan(const TreePlan& p, hipStream_t s) {
-  hipLaunchKernelGGL(tree_plan_kernel, dim3(1 + (p.batch + 15) / 16), dim3(1024), 0, s, p);
+hipError_t launch_tree_plan(const TreeArgs& p, TreeItem* out, hipStream_t s) {
+  hipLaunchKernelGGL(tree_plan_kernel, dim3(1), dim3(1024), 0, s, p, out);
   return hipGetLastError();
 }
 
-// An item's record, every field checked before it addresses memory: where the
-// device arrays disagree with the host's plan it may be stale.
-__device__ __forceinline__ bool load_item(const TreeAttn& P, int i, TreeItem& it) {
-  it = P.item[i];
+// Item i of the step, for a whole wavefront; false if there is none (an empty tree,
+// or device arrays that disagree with the host's plan: bit 8). Where no tree is
+// split, item i is tree i. Otherwise, up to TREE_SCAN sequences, each wavefront
+// finds it by itself, four sequences per lane: one round of memory instead of a
+// launch in front of the step (48 trees 7 us, one tree 5 us). Larger batches read
+// the plan kernel's records, every field checked before it addresses memory, since
+// one that the plan did not write may be stale.
+__device__ __forceinline__ bool find_item(const TreeArgs& P, int i, TreeItem& it) {
+  bool ok = false;
+  it = TreeItem{};
+  if (P.n_rows == 0) {
+    const TreeSpan s = tree_span(P, i, true);
+    if (uniform(s.n) == 0) return false;
+    it = split_of(P, s, i, 0, 0);
+    ok = it.splits == 1;
+  } else if (P.item) {
+    it = P.item[i];
+    ok = it.b >= 0 && it.b < P.batch && it.n > 0 && it.n <= TREE_MAX_NODES && it.t0 >= 0 &&
+         it.t0 <= P.n_tokens - it.n && it.len >= 0 && it.pg0 >= 0 && it.pg0 < it.pg1 && it.pg1 <= P.max_pages &&
+         it.splits > 0 && (it.splits == 1 || (it.row0 >= 0 && it.row0 <= P.n_rows - it.n));
+  } else {
+    const int lane = lane_id();
+    TreeSpan s[TREE_SCAN / 64];
+#pragma unroll
+    for (int c = 0; c < TREE_SCAN / 64; ++c) s[c] = tree_span(P, 64 * c + lane, false);
+    int items = 0, rows = 0;
+#pragma unroll
+    for (int c = 0; c < TREE_SCAN / 64; ++c) {
+      if (64 * c >= P.batch) break;
+      const int incl = wave_incl_scan(s[c].splits), rincl = wave_incl_scan(rows_of(s[c]));
+      const uint64_t past = __ballot(items + incl > i);
+      if (!ok && past != 0) {  // uniform
+        const int src = (int)__builtin_ctzll(past);
+        TreeSpan r;
+        r.t0 = __builtin_amdgcn_readlane(s[c].t0, src); r.n = __builtin_amdgcn_readlane(s[c].n, src);
+        r.len = __builtin_amdgcn_readlane(s[c].len, src); r.pages = __builtin_amdgcn_readlane(s[c].pages, src);
+        r.splits = __builtin_amdgcn_readlane(s[c].splits, src);
+        const int k = i - (items + __builtin_amdgcn_readlane(incl, src) - r.splits);
+        it = split_of(P, r, 64 * c + src, rows + __builtin_amdgcn_readlane(rincl, src) - rows_of(r), k);
+        ok = it.splits == 1 || it.row0 <= P.n_rows - it.n;
+      }
+      items += __builtin_amdgcn_readlane(incl, 63);
+      rows += __builtin_amdgcn_readlane(rincl, 63);
+    }
+    if (i == 0) {
+      if ((items != P.n_items || rows != P.n_rows) && lane == 0) set_error(P.err, 8);
+      for (int b = lane; b < P.batch; b += 64) tree_span(P, b, true);  // report spans that do not fit
+    }
+  }
   it.b = uniform(it.b); it.t0 = uniform(it.t0); it.n = uniform(it.n); it.len = uniform(it.len);
   it.pg0 = uniform(it.pg0); it.pg1 = uniform(it.pg1); it.row0 = uniform(it.row0); it.splits = uniform(it.splits);
-  const bool ok = it.b >= 0 && it.b < P.batch && it.n > 0 && it.n <= TREE_MAX_NODES && it.t0 >= 0 &&
-                  it.t0 + it.n <= P.n_tokens && it.len >= 0 && it.pg0 >= 0 && it.pg0 < it.pg1 &&
-                  it.pg1 <= P.max_pages && (it.splits == 1 || (it.row0 >= 0 && it.row0 + it.n <= P.n_rows));
   if (!ok && lane_id() == 0) set_error(P.err, 8);
   return ok;
+}
+
+// The ancestors of a tree's nodes by one wavefront, lane i = node i: bit a of
+// `seen` is set if node a is an ancestor of i, or i itself, inside i's window;
+// depth counts all ancestors. By pointer doubling: after round r lane i has the
+// union of its first 2^r ancestors and points 2^r steps up. A parent outside
+// [-1, i) raises bit 64 and counts as -1.
+struct Nodes {
+  uint64_t seen;
+  int depth;
+};
+__device__ __forceinline__ Nodes nodes_of(const TreeArgs& P, const TreeItem& it) {
+  const int lane = lane_id();
+  int up = lane < it.n ? P.parents[it.t0 + lane] : -1;
+  if (up < -1 || up >= lane) {
+    if (lane < it.n) set_error(P.err, 64);
+    up = -1;
+  }
+  const int parent = up;
+  Nodes d;
+  d.seen = 1ull << lane;
+#pragma unroll
+  for (int r = 0; r < 6; ++r) {
+    if (__ballot(up >= 0) == 0) break;
+    const int from = max(up, 0);
+    const uint32_t lo = __shfl((uint32_t)d.seen, from, 64), hi = __shfl((uint32_t)(d.seen >> 32), from, 64);
+    const int next = __shfl(up, from, 64);
+    d.seen |= up >= 0 ? (uint64_t)hi << 32 | lo : 0;
+    up = up >= 0 ? next : -1;
+  }
+  d.depth = __popcll(d.seen) - 1;
+  // a window shorter than the branch drops the ancestors that lie window or more steps up
+  if (P.window > 0 && __ballot(d.depth >= P.window) != 0) {
+    uint64_t near = 1ull << lane;
+    int a = parent;
+    for (int k = 1; k < TREE_MAX_NODES; ++k) {
+      near |= a >= 0 && k < P.window ? 1ull << (a & 63) : 0;
+      const int next = __shfl(parent, max(a, 0), 64);
+      a = a >= 0 ? next : -1;
+    }
+    d.seen = near;
+  }
+  return d;
+}
+
+// What the combine needs to know of a tree's tokens: the first partial row, the
+// rows from one split to the next, and the splits. Written by one wavefront of the
+// tree's first split, in steps that have a combine.
+__device__ __forceinline__ void write_rows(const TreeAttn& P, const TreeItem& it) {
+  const int lane = lane_id();
+  if (P.n_rows > 0 && it.pg0 == first_page(it.len, P.window) && lane < it.n)
+    P.tok[it.t0 + lane] = make_int4(it.row0 + lane, it.n, it.splits, 0);
 }
 
 // ---------------------------------------------------------------------------
@@ -188,12 +246,20 @@ struct Sight {
     const bool old = slot >= lo, mine = (a < n) & ((seen >> (a & 63) & 1) != 0);
     return a < 0 ? old : mine;
   }
+  // the same for 32 slots from k0 on, bit i: slot k0 + i
+  __device__ __forceinline__ uint32_t keys(int k0, int len) const {
+    const int off = k0 - len, left = lo - k0;  // first node, first committed key in sight
+    const uint64_t nodes = off >= 0 ? (off < 64 ? seen >> off : 0) : (off > -32 ? seen << -off : 0);
+    const uint32_t old = off >= 0 ? 0u : off > -32 ? (1u << -off) - 1u : ~0u;
+    return (uint32_t)nodes | (old & ~(left <= 0 ? 0u : left < 32 ? (1u << left) - 1u : ~0u));
+  }
 };
-__device__ __forceinline__ Sight sight_of(const TreeAttn& P, const TreeItem& it, int node) {
-  const TreeNode d = P.node[it.t0 + node];
+__device__ __forceinline__ Sight sight_of(const TreeAttn& P, const TreeItem& it, const Nodes& nodes, int node) {
+  const uint32_t lo = __shfl((uint32_t)nodes.seen, node, 64), hi = __shfl((uint32_t)(nodes.seen >> 32), node, 64);
+  const int depth = __shfl(nodes.depth, node, 64);
   Sight s;
-  s.lo = P.window > 0 ? it.len + d.depth - P.window + 1 : 0;
-  s.seen = d.seen;
+  s.lo = P.window > 0 ? it.len + depth - P.window + 1 : 0;
+  s.seen = (uint64_t)hi << 32 | lo;
   return s;
 }
 
@@ -208,15 +274,16 @@ template <typename T, int D>
 __global__ __launch_bounds__(256) void tree_attn_kernel(TreeAttn P, int tiles) {
   const int lane = lane_id(), hl = lane & 15, grp = lane >> 4;
   const unsigned id = blockIdx.x * 4 + uniform(threadIdx.x >> 6), hkv = P.hkv;
-  const int g = id % hkv, tile = id / hkv % (unsigned)tiles, i = id / hkv / (unsigned)tiles;
-  if (i >= P.n_items) return;  // no barriers below
+  const int g = id % hkv, tile = id / hkv % (unsigned)tiles, item = id / hkv / (unsigned)tiles;
+  if (item >= P.n_items) return;  // no barriers below
   TreeItem it;
-  if (!load_item(P, i, it)) return;
+  if (!find_item(P, item, it)) return;
   const int G = P.hq / P.hkv, cols = it.n * G;
   if (16 * tile >= cols) return;
   const int c = 16 * tile + hl, node = min(c / G, it.n - 1), head = g * G + c % G;
   const bool valid = c < cols;
-  const Sight sight = sight_of(P, it, node);
+  const Sight sight = sight_of(P, it, nodes_of(P, it), node);
+  if (g == 0 && tile == 0) write_rows(P, it);
   Frag<T> qf[D / 32];
   const T* qb = reinterpret_cast<const T*>(P.q) + ((int64_t)(it.t0 + node) * P.hq + head) * D + 8 * grp;
 #pragma unroll
@@ -330,21 +397,12 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(TreeAttn P, int tiles) {
     for (int r = 0; r < 4; ++r) Elem<T>::store(o, 16 * n + r, l == 0.f ? 0.f : f * acc[n][r] / l);
 }
 
-template <typename T, int D>
-static hipError_t tree_attn_impl(const TreeAttn& p, hipStream_t s) {
-  const int tiles = (p.max_nodes * (p.hq / p.hkv) + 15) / 16;
-  const int64_t waves = (int64_t)p.n_items * p.hkv * tiles;
-  if (waves > 0x7FFFFFFF) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((tree_attn_kernel<T, D>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, p, tiles);
-  return hipGetLastError();
-}
-
 // ---------------------------------------------------------------------------
 // attend, bf16 with head dim 64: 64 columns per wavefront
 // ---------------------------------------------------------------------------
 
 // A workgroup of NC wavefronts owns one split of one tree and KV head; each
-// wavefront holds 64 columns, two tiles of 32. The pages go straight to LDS, two
+// wavefront holds NT tiles of 32 columns. The pages go straight to LDS, two
 // (32 keys) a step through TRS stages, once for all NC wavefronts. Per step a
 // wavefront forms S^T = K Q^T as a 32 x 32 tile per 32 columns and accumulates
 // O^T += V^T P^T from it: lane l holds column l % 32 and, with h = l / 32, keys
@@ -354,12 +412,149 @@ static hipError_t tree_attn_impl(const TreeAttn& p, hipStream_t s) {
 // The maximum of a column is raised only when a lane's share of a step's weights
 // would pass 2^8, so that most steps have no cross-lane step and no rescale.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) void* lds_void_t;
 
-template <int NC, int TRS>
-__global__ __launch_bounds__(64 * NC, 2) void tree_attn_wide_kernel(TreeAttn P, int tiles) {
+// O^T tiles of 32 x 32 products: lane l holds column l % 32 and, with h = l / 32, the
+// dims (or keys) 8 q + 4 h + r in element 4 q + r.
+
+// keys that are not in sight get a score of -inf; `mine`: the step's keys from the
+// lane's first one on
+__device__ __forceinline__ void hide(f32x16& t, uint32_t mine) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {  // all ones where the key is in sight: a bit-field extract and a bit select
+    const uint32_t in = (uint32_t)((int32_t)(mine << (31 - (8 * (e >> 2) + (e & 3)))) >> 31);
+    t[e] = __uint_as_float((in & __float_as_uint(t[e])) | (~in & 0xFF800000u));
+  }
+}
+// a column's largest score of a step, over both of its lanes
+__device__ __forceinline__ float largest(const f32x16& t) {
+  float m = t[0];
+#pragma unroll
+  for (int e = 1; e < 16; ++e) m = vmax(m, t[e]);
+  const uint32_t u = __float_as_uint(m);
+  auto sw = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return vmax(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+}
+// weights 2^(score scale - m), rounded to bf16 as the value product takes them (its
+// operand type), and their sum after that rounding, so that the quotient is of the
+// same weights
+__device__ __forceinline__ float weigh(const f32x16& t, float scale_log2, float m, u32x4_t (&pw)[2]) {
+  float sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < 16; e += 2) {
+    const float p0 = __builtin_amdgcn_exp2f(fmaf(t[e], scale_log2, -m));
+    const float p1 = __builtin_amdgcn_exp2f(fmaf(t[e + 1], scale_log2, -m));
+    const uint32_t w = pack_bf16(p0, p1);
+    pw[e >> 3][(e & 7) >> 1] = w;
+    sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w), __builtin_bit_cast(bf16x2_t, 0x3F803F80u), sum, false);
+  }
+  return sum;
+}
+// Value fragments of a step with masked keys: a weight of zero times a value that is
+// not finite would not be zero, so such values are set to zero; true for the whole
+// wavefront if there were any (add_nonfinite gives them back to the columns that
+// see them).
+__device__ __forceinline__ bool drop_nonfinite(u32x4_t (&vf)[2][2]) {
+  const u16x2_t full = {0x7F80, 0x7F80}, one = {1, 1};
+  u16x2_t top = {0, 0};  // the largest exponent field in either half
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+#pragma unroll
+    for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2_t, vf[p][dt][i] & 0x7F807F80u));
+  const bool odd = top.x == 0x7F80u || top.y == 0x7F80u;
+  if (__builtin_amdgcn_ballot_w64(odd) == 0) return false;
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+#pragma unroll
+    for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {  // halves times 0 where the exponent is full, else times 1
+        const uint32_t w = vf[p][dt][i];
+        const u16x2_t keep = __builtin_elementwise_min(full - __builtin_bit_cast(u16x2_t, w & 0x7F807F80u), one);
+        vf[p][dt][i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(u16x2_t, w) * keep);
+      }
+  return true;
+}
+// The steps with masked keys once more, for values that are not finite: added to the
+// accumulators of the columns that see them, which makes those infinite or NaN as
+// any positive weight does. Steps without masked keys need no such care.
+template <int NT>
+__device__ __forceinline__ void add_nonfinite(const TreeAttn& P, const TreeItem& it, int g, const Sight (&sight)[NT],
+                                              const bool (&valid)[NT], int h, f32x16 (&acc)[2][NT]) {
+  constexpr int D = 64;
+  const int32_t* ptab = P.page_table + (int64_t)it.b * P.max_pages;
+  for (int pg = it.pg0; pg < it.pg1; ++pg) {
+    const int k0 = pg * PAGE, id = uniform(ptab[pg]);
+    if (id < 0 || id >= P.n_pages) continue;
+    // the pages of steps with masked keys, and at most one page more on either side
+    if (k0 + 3 * PAGE <= it.len && !(P.window > 0 && k0 < it.len + it.n - P.window + PAGE) && pg + 2 < it.pg1) {
+      const int before = uniform(ptab[max(pg - 1, it.pg0)]), after = uniform(ptab[pg + 1]);
+      if (before >= 0 && before < P.n_pages && after >= 0 && after < P.n_pages) continue;
+    }
+    const bf16* page = reinterpret_cast<const bf16*>(P.v_pool) + ((int64_t)id * P.hkv + g) * PAGE * D;
+    for (int slot = 0; slot < PAGE; ++slot)
+#pragma unroll
+      for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const uint16_t bits = page[v_off(slot, 32 * dt + 8 * (e >> 2) + 4 * h + (e & 3))].bits;
+          const bool bad = (bits & 0x7F80u) == 0x7F80u;
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+            acc[dt][j][e] += bad & valid[j] & sight[j].key(k0 + slot, it.len, it.n) ? bf16_to_f32(bits) : 0.f;
+        }
+  }
+}
+// the lane's dims of each column: a partial row, or o with the sink
+template <int NT>
+__device__ __forceinline__ void finish(const TreeAttn& P, const TreeItem& it, const int (&node)[NT], const int (&head)[NT],
+                                       const bool (&valid)[NT], int h, const float (&m_run)[NT], const float (&l)[NT],
+                                       const f32x16 (&acc)[2][NT]) {
+  constexpr int D = 64;
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const uint32_t u = __float_as_uint(l[j]);
+    auto sw = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    float l_tot = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    if (!valid[j]) continue;
+    if (it.splits > 1) {
+      const int64_t row = (int64_t)(it.row0 + node[j]) * P.hq + head[j];
+      if (h == 0) *reinterpret_cast<float2*>(P.part_ml + 2 * row) = make_float2(m_run[j], l_tot);
+#pragma unroll
+      for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<float4*>(P.part_acc + row * D + 32 * dt + 8 * q + 4 * h) =
+              make_float4(acc[dt][j][4 * q], acc[dt][j][4 * q + 1], acc[dt][j][4 * q + 2], acc[dt][j][4 * q + 3]);
+      continue;
+    }
+    float f = 1.0f;
+    if (P.sinks) {
+      const float sk = P.sinks[head[j]] * LOG2E, M = fmaxf(m_run[j], sk);
+      f = m_run[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[j] - M);
+      l_tot = l_tot * f + __builtin_amdgcn_exp2f(sk - M);
+    }
+    const float inv = l_tot == 0.f ? 0.f : f / l_tot;
+    bf16* o = reinterpret_cast<bf16*>(P.o) + ((int64_t)(it.t0 + node[j]) * P.hq + head[j]) * D + 4 * h;
+#pragma unroll
+    for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        store4(o + 32 * dt + 8 * q, make_float4(acc[dt][j][4 * q] * inv, acc[dt][j][4 * q + 1] * inv,
+                                                acc[dt][j][4 * q + 2] * inv, acc[dt][j][4 * q + 3] * inv));
+  }
+}
+
+template <int NC, int NT, int TRS>
+__global__ __launch_bounds__(64 * NC, NT == 1 ? 4 : 2) void tree_attn_wide_kernel(TreeAttn P, int tiles) {
   constexpr int D = 64, PE = PAGE * D, PB = 2 * PE;  // elements and bytes of a page of one KV head
   constexpr int LD = 8 / NC;                         // 1 KB loads per wavefront and step
+  // up to 128 columns no other workgroup reads the pages: the streaming policy (5% at 48 trees of 8-16 nodes)
+  constexpr int POLICY = NC * NT <= 4 ? 2 : 0;
   static_assert(TRS % 2 == 0 && TRS <= 6 && 8 % NC == 0, "stages alternate between two score sets");
   __shared__ __align__(1024) uint8_t s0[4 * PB];
   __shared__ __align__(1024) uint8_t s1[4 * PB];
@@ -371,30 +566,36 @@ __global__ __launch_bounds__(64 * NC, 2) void tree_attn_wide_kernel(TreeAttn P, 
     return s == 0 ? s0 : s == 1 ? s1 : s == 2 ? s2 : s == 3 ? s3 : s == 4 ? s4 : s5;
   };
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const unsigned hkv = P.hkv;
-  const int g = blockIdx.x % hkv, tile = blockIdx.x / hkv % (unsigned)tiles, item = blockIdx.x / hkv / (unsigned)tiles;
+  // workgroups are dealt to the eight XCDs in turn: the column tiles of one split and head go to the same one
+  const unsigned hkv = P.hkv, slot = blockIdx.x >> 3;
+  const unsigned pair = slot / (unsigned)tiles * 8 + (blockIdx.x & 7);
+  const int tile = slot % (unsigned)tiles, g = pair % hkv, item = pair / hkv;
+  if (item >= P.n_items) return;
   TreeItem it;
-  if (!load_item(P, item, it)) return;
+  if (!find_item(P, item, it)) return;  // uniform over the workgroup
   const int G = P.hq / P.hkv, cols = it.n * G;
-  if (64 * NC * tile >= cols) return;
-  const int c0 = 64 * (NC * tile + wave);
+  if (32 * NT * NC * tile >= cols) return;
+  const int c0 = 32 * NT * (NC * tile + wave);
   const bool busy = c0 < cols;  // wave-uniform; a wavefront without columns only loads
   const int32_t* ptab = P.page_table + (int64_t)it.b * P.max_pages;
   const int n_steps = (it.pg1 - it.pg0 + 1) / 2;
 
-  // this lane's column in each of the wavefront's two tiles
+  const Nodes nodes = nodes_of(P, it);
+  if (g == 0 && tile == 0 && wave == 0) write_rows(P, it);
+
+  // this lane's column in each of the wavefront's tiles
   const int fc = lane & 31, h = lane >> 5;
-  int node[2], head[2];
-  bool valid[2];
-  Sight sight[2];
-  Frag<bf16> qf[2][4];
+  int node[NT], head[NT];
+  bool valid[NT];
+  Sight sight[NT];
+  Frag<bf16> qf[NT][4];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
+  for (int j = 0; j < NT; ++j) {
     const int c = c0 + 32 * j + fc;
     valid[j] = c < cols;
     node[j] = min(c / G, it.n - 1);
     head[j] = g * G + c % G;
-    sight[j] = sight_of(P, it, node[j]);
+    sight[j] = sight_of(P, it, nodes, node[j]);
     const bf16* qp = reinterpret_cast<const bf16*>(P.q) + ((int64_t)(it.t0 + node[j]) * P.hq + head[j]) * D + 8 * h;
 #pragma unroll
     for (int cc = 0; cc < 4; ++cc) {
@@ -421,7 +622,10 @@ __global__ __launch_bounds__(64 * NC, 2) void tree_attn_wide_kernel(TreeAttn P, 
     good = id >= 0 && id < P.n_pages;
     return good ? id : 0;
   };
+  // request a step's pages; past the split's end the loads have no range and touch no memory, so that every
+  // step counts the same number of them
   auto request = [&](uint8_t* stg, int step) __attribute__((always_inline)) {
+    const int range = step < n_steps ? PB : 0;
 #pragma unroll
     for (int u = 0; u < LD; ++u) {
       const int w = wave * LD + u;
@@ -429,18 +633,19 @@ __global__ __launch_bounds__(64 * NC, 2) void tree_attn_wide_kernel(TreeAttn P, 
       const int id = page_of(step, (w >> 1) & 1, good);
       const uint8_t* pool = reinterpret_cast<const uint8_t*>(w < 4 ? P.k_pool : P.v_pool) + (int64_t)g * PB;
       const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
-          const_cast<uint8_t*>(pool) + id * page_bytes, 0, PB, 0x00020000);
+          const_cast<uint8_t*>(pool) + id * page_bytes, 0, range, 0x00020000);
       const uint32_t at = 1024u * (w & 1) + 16u * lane;
       const uint32_t vo = w < 4 ? at : at ^ (((at >> 9) & 1u) << 7);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t)(stg + 1024 * w), 16, vo, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t)(stg + 1024 * w), 16, vo, 0, 0, POLICY);
     }
   };
 
   constexpr float WEIGHT_LIMIT = 0x1p8f;       // of a lane's 16 weights in a step
-  float m_run[2], m_sub[2], limit[2], l[2];    // limit: -inf until a key is visible
-  f32x16 acc[2][2];                            // [dim tile][column tile]
+  bool odd = false;  // values that are not finite were dropped
+  float m_run[NT], m_sub[NT], limit[NT], l[NT];    // limit: -inf until a key is visible
+  f32x16 acc[2][NT];                           // [dim tile][column tile]
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
+  for (int j = 0; j < NT; ++j) {
     m_run[j] = -INFINITY;
     m_sub[j] = 0.f;
     limit[j] = -INFINITY;
@@ -456,7 +661,7 @@ __global__ __launch_bounds__(64 * NC, 2) void tree_attn_wide_kernel(TreeAttn P, 
   const uint32_t vbase = (fc >> 4) * 512 + (fc & 15) * 8 + (((uint32_t)h ^ ((fc >> 4) & 1)) << 7);
 
   struct Scores {
-    f32x16 t[2];
+    f32x16 t[NT];
   };
   auto load_keys = [&](u32x4_t (&kf)[4], const uint8_t* stg) __attribute__((always_inline)) {
 #pragma unroll
@@ -464,23 +669,20 @@ __global__ __launch_bounds__(64 * NC, 2) void tree_attn_wide_kernel(TreeAttn P, 
   };
   auto scores = [&](Scores& sc, const u32x4_t (&kf)[4]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) sc.t[j][e] = 0.f;
 #pragma unroll
     for (int cc = 0; cc < 4; ++cc)
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int j = 0; j < NT; ++j)
         sc.t[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[cc]),
                                                           __builtin_bit_cast(bf16x8_t, qf[j][cc].v), sc.t[j], 0, 0, 0);
   };
-  // the keys of a step that a column sees, bit i: key i
-  auto visible = [&](int j, int k0, uint32_t pages) __attribute__((always_inline)) {
-    const int off = k0 - it.len, lo = sight[j].lo - k0;  // first node, first committed key in sight
-    const uint64_t nodes = off >= 0 ? (off < 64 ? sight[j].seen >> off : 0) : (off > -32 ? sight[j].seen << -off : 0);
-    const uint32_t old = off >= 0 ? 0u : off > -32 ? (1u << -off) - 1u : ~0u;
-    const uint32_t left = lo <= 0 ? 0u : lo < 32 ? (1u << lo) - 1u : ~0u;
-    return valid[j] ? ((uint32_t)nodes | (old & ~left)) & pages : ~0u;
+  auto start_at = [&](int j, float m) __attribute__((always_inline)) {
+    m_run[j] = m;
+    m_sub[j] = m == -INFINITY ? 0.f : m;  // masked scores give 2^-inf = 0
+    limit[j] = m == -INFINITY ? -INFINITY : WEIGHT_LIMIT;
   };
   // a step's softmax and value products from its scores, and the scores of the next step
   auto attend = [&](Scores& sc, Scores& sn, const uint8_t* stg, const uint8_t* nxt, int step) __attribute__((always_inline)) {
@@ -492,68 +694,51 @@ __global__ __launch_bounds__(64 * NC, 2) void tree_attn_wide_kernel(TreeAttn P, 
     const int pg = it.pg0 + 2 * step, k0 = pg * PAGE;
     const bool second = pg + 1 < it.pg1;
     const bool edge = k0 + 2 * PAGE > it.len || (P.window > 0 && k0 < it.len + it.n - P.window) || !ok[0] || !ok[1] || !second;
-    uint32_t vis[2];
+    uint32_t vis[NT];
     if (__builtin_expect(edge, 0)) {  // wave-uniform; the empty asm keeps it a branch
       asm volatile("");
       if ((!ok[0] || (!ok[1] && second)) && lane == 0) set_error(P.err, 1);
       const uint32_t pages = (ok[0] ? 0xFFFFu : 0u) | (ok[1] && second ? 0xFFFF0000u : 0u);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        vis[j] = visible(j, k0, pages);
-        const uint32_t mine = vis[j] >> (4 * h);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sc.t[j][e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? sc.t[j][e] : -INFINITY;
+      for (int j = 0; j < NT; ++j) {
+        vis[j] = valid[j] ? sight[j].keys(k0, it.len) & pages : ~0u;
+        hide(sc.t[j], vis[j] >> (4 * h));
       }
     }
-    u32x4_t pw[2][2];  // [column tile][page]: the weights, packed
-    float sum[2];
+    u32x4_t pw[NT][2];  // [column tile][page]: the weights, packed
+    float sum[NT];
     auto weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        sum[j] = 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(sc.t[j][e], P.scale_log2, -m_sub[j]));
-          const float p1 = __builtin_amdgcn_exp2f(fmaf(sc.t[j][e + 1], P.scale_log2, -m_sub[j]));
-          const uint32_t w = pack_bf16(p0, p1);
-          pw[j][e >> 3][(e & 7) >> 1] = w;
-          sum[j] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w), __builtin_bit_cast(bf16x2_t, 0x3F803F80u), sum[j], false);
-        }
-      }
+      for (int j = 0; j < NT; ++j) sum[j] = weigh(sc.t[j], P.scale_log2, m_sub[j], pw[j]);
     };
     __builtin_amdgcn_sched_barrier(0);
     scores(sn, kf);
     weights();
-    // the next scores' eight products among the 96 vector instructions of the weights
+    // the next scores' products among the vector instructions of the weights, 12 each
 #define TREE_MIX                                      \
   __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  \
   __builtin_amdgcn_sched_group_barrier(0x402, 12, 0);
-    TREE_MIX TREE_MIX TREE_MIX TREE_MIX TREE_MIX TREE_MIX TREE_MIX TREE_MIX
+    TREE_MIX TREE_MIX TREE_MIX TREE_MIX
+    if constexpr (NT == 2) { TREE_MIX TREE_MIX TREE_MIX TREE_MIX }
 #undef TREE_MIX
     // The maximum only has to keep the weights in range, so it is raised when a step's sum says that they are
     // not, and until a column has seen a key; the weights are then formed again.
-    const bool raise = sum[0] > limit[0] || sum[1] > limit[1];
+    bool raise = false;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) raise |= sum[j] > limit[j];
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(raise) != 0, 0)) {  // wave-uniform (kept a branch)
       asm volatile("");
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        float mloc = sc.t[j][0];
-#pragma unroll
-        for (int e = 1; e < 16; ++e) mloc = vmax(mloc, sc.t[j][e]);
-        const uint32_t u = __float_as_uint(mloc);
-        auto sw = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-        const float mstep = vmax(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * P.scale_log2;
+      for (int j = 0; j < NT; ++j) {
         // a column's own lanes decide, so that its bits do not depend on the columns beside it
         const uint32_t o = sum[j] > limit[j];
         auto so = __builtin_amdgcn_permlane32_swap(o, o, false, false);
-        const float m_new = (so[0] | so[1]) ? fmaxf(m_run[j], mstep) : m_run[j];
+        const float m_new = (so[0] | so[1]) ? fmaxf(m_run[j], largest(sc.t[j]) * P.scale_log2) : m_run[j];
         const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[j] - m_new);
         l[j] *= alpha;
 #pragma unroll
         for (int dt = 0; dt < 2; ++dt) acc[dt][j] *= alpha;
-        m_run[j] = m_new;
-        m_sub[j] = m_new == -INFINITY ? 0.f : m_new;  // masked scores give 2^-inf = 0
-        limit[j] = m_new == -INFINITY ? -INFINITY : WEIGHT_LIMIT;
+        start_at(j, m_new);
       }
       weights();
     }
@@ -568,38 +753,10 @@ __global__ __launch_bounds__(64 * NC, 2) void tree_attn_wide_kernel(TreeAttn P, 
       }
     if (__builtin_expect(edge, 0)) {
       asm volatile("");
-      bool odd = false;
-#pragma unroll
-      for (int p = 0; p < 2; ++p)
-#pragma unroll
-        for (int dt = 0; dt < 2; ++dt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t w = vf[p][dt][i];
-            odd |= drop_nonfinite(w);
-            vf[p][dt][i] = w;
-          }
-      if (__builtin_amdgcn_ballot_w64(odd) != 0) {  // rare: values that are not finite, for the columns that see them
-        for (int key = 0; key < 2 * PAGE; ++key) {
-          const uint8_t* page = stg + (2 + (key >> 4)) * PB;
-          const int slot = key & 15;
-#pragma unroll
-          for (int dt = 0; dt < 2; ++dt)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int dim = 32 * dt + 8 * (e >> 2) + 4 * h + (e & 3);
-              const uint32_t at = 2 * v_off(slot, dim);
-              const uint16_t bits = *reinterpret_cast<const uint16_t*>(page + (at ^ (((at >> 9) & 1u) << 7)));
-              const bool bad = (bits & 0x7F80u) == 0x7F80u;
-#pragma unroll
-              for (int j = 0; j < 2; ++j)
-                acc[dt][j][e] += bad && (vis[j] >> key & 1) ? bf16_to_f32(bits) : 0.f;
-            }
-        }
-      }
+      odd |= drop_nonfinite(vf);
     }
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < NT; ++j) {
       l[j] += sum[j];
 #pragma unroll
       for (int p = 0; p < 2; ++p)
@@ -661,63 +818,236 @@ __global__ __launch_bounds__(64 * NC, 2) void tree_attn_wide_kernel(TreeAttn P, 
   }
   __builtin_amdgcn_s_waitcnt(0);  // no load into LDS may outlive the workgroup
 
-  // this lane's dims 32 dt + 8 q + 4 h .. + 3 of each column: a partial row, or o with the sink
+  if (odd) add_nonfinite<NT>(P, it, g, sight, valid, h, acc);
+  finish<NT>(P, it, node, head, valid, h, m_run, l, acc);
+}
+
+// The same products for few columns: one wavefront per split, KV head and NT x 32
+// columns, its pages straight to registers, two steps in flight. Nothing is shared,
+// so there is no LDS and no barrier, and the wavefronts of a SIMD hide each other's
+// loads and products.
+template <int NT>
+__global__ __launch_bounds__(64, NT == 1 ? 3 : 2) void tree_attn_narrow_kernel(TreeAttn P, int tiles) {
+  constexpr int D = 64, PE = PAGE * D;
+  const int lane = lane_id();
+  const unsigned hkv = P.hkv, slot = blockIdx.x >> 3;
+  const unsigned pair = slot / (unsigned)tiles * 8 + (blockIdx.x & 7);
+  const int tile = slot % (unsigned)tiles, g = pair % hkv, item = pair / hkv;
+  if (item >= P.n_items) return;
+  TreeItem it;
+  if (!find_item(P, item, it)) return;
+  const int G = P.hq / P.hkv, cols = it.n * G, c0 = 32 * NT * tile;
+  if (c0 >= cols) return;
+  const int32_t* ptab = P.page_table + (int64_t)it.b * P.max_pages;
+  const int n_steps = (it.pg1 - it.pg0 + 1) / 2;
+  const int64_t page_elems = (int64_t)P.hkv * PE;
+  const bf16* kpool = reinterpret_cast<const bf16*>(P.k_pool) + (int64_t)g * PE;
+  const bf16* vpool = reinterpret_cast<const bf16*>(P.v_pool) + (int64_t)g * PE;
+  const int fc = lane & 31, h = lane >> 5;
+
+  // page ids of steps base .. base + 31, lane i: page pg0 + 2 base + i
+  auto ids_of = [&](int base) __attribute__((always_inline)) {
+    return ptab[min(it.pg0 + 2 * base + lane, it.pg1 - 1)];
+  };
+  int ids = ids_of(0);
+  struct Step {
+    u32x4_t k[4];     // key fc of the step, dims 8 h .. of each 16-dim chunk
+    u32x2_t v[2][4];  // [page][2 dim tile + half]: dim fc of a tile of 32, value rows 4 h .. and 8 + 4 h ..
+    bool ok[2];
+  };
+  const uint32_t ko = (h * 16 + (fc & 15)) * 8, vo = (fc >> 4) * 256 + (fc & 15) * 4 + h * 64;
+  auto fetch = [&](Step& st, int step, int at) __attribute__((always_inline)) {  // `at`: the step's place in ids
+    int64_t off[2];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const uint32_t u = __float_as_uint(l[j]);
-    auto sw = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    float l_tot = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-    if (!valid[j]) continue;
-    if (it.splits > 1) {
-      const int64_t row = (int64_t)(it.row0 + node[j]) * P.hq + head[j];
-      if (h == 0) *reinterpret_cast<float2*>(P.part_ml + 2 * row) = make_float2(m_run[j], l_tot);
-#pragma unroll
-      for (int dt = 0; dt < 2; ++dt)
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          *reinterpret_cast<float4*>(P.part_acc + row * D + 32 * dt + 8 * q + 4 * h) =
-              make_float4(acc[dt][j][4 * q], acc[dt][j][4 * q + 1], acc[dt][j][4 * q + 2], acc[dt][j][4 * q + 3]);
-      continue;
+    for (int p = 0; p < 2; ++p) {
+      const int id = __builtin_amdgcn_readlane(ids, 2 * at + p);
+      const bool good = id >= 0 && id < P.n_pages;
+      st.ok[p] = good && it.pg0 + 2 * step + p < it.pg1;
+      off[p] = (good ? id : 0) * page_elems;
     }
-    float f = 1.0f;
-    if (P.sinks) {
-      const float sk = P.sinks[head[j]] * LOG2E, M = fmaxf(m_run[j], sk);
-      f = m_run[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[j] - M);
-      l_tot = l_tot * f + __builtin_amdgcn_exp2f(sk - M);
+    const bf16* kp = kpool + (fc < 16 ? off[0] : off[1]) + ko;
+#pragma unroll
+    for (int cc = 0; cc < 4; ++cc) st.k[cc] = ld_stream16(kp + 256 * cc);
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) st.v[p][i] = ld_stream8(vpool + off[p] + vo + 512 * (i >> 1) + 128 * (i & 1));
+  };
+
+  const Nodes nodes = nodes_of(P, it);
+  if (g == 0 && tile == 0) write_rows(P, it);
+  int node[NT], head[NT];
+  bool valid[NT];
+  Sight sight[NT];
+  Frag<bf16> qf[NT][4];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int c = c0 + 32 * j + fc;
+    valid[j] = c < cols;
+    node[j] = min(c / G, it.n - 1);
+    head[j] = g * G + c % G;
+    sight[j] = sight_of(P, it, nodes, node[j]);
+    const bf16* qp = reinterpret_cast<const bf16*>(P.q) + ((int64_t)(it.t0 + node[j]) * P.hq + head[j]) * D + 8 * h;
+#pragma unroll
+    for (int cc = 0; cc < 4; ++cc) {
+      qf[j][cc].load(qp + 16 * cc);
+      qf[j][cc].keep_if(valid[j]);
     }
-    const float inv = l_tot == 0.f ? 0.f : f / l_tot;
-    bf16* o = reinterpret_cast<bf16*>(P.o) + ((int64_t)(it.t0 + node[j]) * P.hq + head[j]) * D + 4 * h;
+  }
+  constexpr float WEIGHT_LIMIT = 0x1p8f;
+  bool odd = false;  // values that are not finite were dropped
+  float m_run[NT], m_sub[NT], limit[NT], l[NT];
+  f32x16 acc[2][NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    m_run[j] = -INFINITY;
+    m_sub[j] = 0.f;
+    limit[j] = -INFINITY;
+    l[j] = 0.f;
 #pragma unroll
     for (int dt = 0; dt < 2; ++dt)
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        store4(o + 32 * dt + 8 * q, make_float4(acc[dt][j][4 * q] * inv, acc[dt][j][4 * q + 1] * inv,
-                                                acc[dt][j][4 * q + 2] * inv, acc[dt][j][4 * q + 3] * inv));
+      for (int e = 0; e < 16; ++e) acc[dt][j][e] = 0.f;
   }
+  auto attend = [&](Step& st, int step) __attribute__((always_inline)) {
+    f32x16 sc[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[j][e] = 0.f;
+#pragma unroll
+      for (int cc = 0; cc < 4; ++cc)
+        sc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, st.k[cc]),
+                                                        __builtin_bit_cast(bf16x8_t, qf[j][cc].v), sc[j], 0, 0, 0);
+    }
+    const int pg = it.pg0 + 2 * step, k0 = pg * PAGE;
+    const bool edge = k0 + 2 * PAGE > it.len || (P.window > 0 && k0 < it.len + it.n - P.window) || !st.ok[0] || !st.ok[1];
+    uint32_t vis[NT];
+    if (__builtin_expect(edge, 0)) {
+      asm volatile("");
+      if ((!st.ok[0] || (!st.ok[1] && pg + 1 < it.pg1)) && lane == 0) set_error(P.err, 1);
+      const uint32_t pages = (st.ok[0] ? 0xFFFFu : 0u) | (st.ok[1] ? 0xFFFF0000u : 0u);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        vis[j] = valid[j] ? sight[j].keys(k0, it.len) & pages : ~0u;
+        hide(sc[j], vis[j] >> (4 * h));
+      }
+    }
+    u32x4_t pw[NT][2];
+    float sum[NT];
+    auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) sum[j] = weigh(sc[j], P.scale_log2, m_sub[j], pw[j]);
+    };
+    weights();
+    bool raise = false;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) raise |= sum[j] > limit[j];
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(raise) != 0, 0)) {
+      asm volatile("");
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const uint32_t o = sum[j] > limit[j];
+        auto so = __builtin_amdgcn_permlane32_swap(o, o, false, false);
+        const float m_new = (so[0] | so[1]) ? fmaxf(m_run[j], largest(sc[j]) * P.scale_log2) : m_run[j];
+        const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[j] - m_new);
+        l[j] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt) acc[dt][j] *= alpha;
+        m_run[j] = m_new;
+        m_sub[j] = m_new == -INFINITY ? 0.f : m_new;
+        limit[j] = m_new == -INFINITY ? -INFINITY : WEIGHT_LIMIT;
+      }
+      weights();
+    }
+    u32x4_t vf[2][2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int dt = 0; dt < 2; ++dt) vf[p][dt] = __builtin_shufflevector(st.v[p][2 * dt], st.v[p][2 * dt + 1], 0, 1, 2, 3);
+    if (__builtin_expect(edge, 0)) {
+      asm volatile("");
+      odd |= drop_nonfinite(vf);
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      l[j] += sum[j];
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt)
+          acc[dt][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf[p][dt]),
+                                                               __builtin_bit_cast(bf16x8_t, pw[j][p]), acc[dt][j], 0, 0, 0);
+    }
+  };
+  // blocks of 30 steps, whose ids and those of the two steps requested ahead sit in one register; a step past
+  // the end reads the last page again and is masked
+  constexpr int BLK = 30;
+  Step a, b;
+  fetch(a, 0, 0);
+  fetch(b, 1, 1);
+  for (int base = 0;;) {
+    const int next = ids_of(base + BLK), stop = min(n_steps, base + BLK);
+    int step = base;
+    for (; step + 1 < stop; step += 2) {
+      attend(a, step);
+      fetch(a, step + 2, step + 2 - base);
+      attend(b, step + 1);
+      fetch(b, step + 3, step + 3 - base);
+    }
+    if (step < stop) attend(a, step);  // an odd number of steps: only at the split's end
+    if (stop == n_steps) break;
+    base = stop;
+    ids = next;
+  }
+  if (odd) add_nonfinite<NT>(P, it, g, sight, valid, h, acc);
+  finish<NT>(P, it, node, head, valid, h, m_run, l, acc);
 }
 
-template <int NC, int TRS>
-static hipError_t tree_wide_impl(const TreeAttn& p, hipStream_t s) {
-  const int cols = p.max_nodes * (p.hq / p.hkv), tiles = (cols + 64 * NC - 1) / (64 * NC);
-  const int64_t blocks = (int64_t)p.n_items * p.hkv * tiles;
-  if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((tree_attn_wide_kernel<NC, TRS>), dim3((unsigned)blocks), dim3(64 * NC), 0, s, p, tiles);
-  return hipGetLastError();
+// The kernel for a step and the columns that one of its wavefronts or workgroups
+// takes. bf16 with head dim 64 has the 32 x 32 products; their loads need 16-byte
+// aligned pools. `cols` is the largest tree's node and head pairs per KV head;
+// `light`: the step's splits leave compute units idle. Measured, 64 query heads on 8
+// KV heads (us):
+//   up to 32 columns, 48 trees of 1-4 nodes behind ~4 K tokens: NARROW1 100, NARROW2 106, WIDE2 136
+//   up to 64, 48 trees of 1-8: NARROW2 114, NARROW1 171, WIDE2 150
+//   up to 128, 48 trees of 8-16: WIDE2 127, WIDE1 140, NARROW2 174; light, one tree of 16 behind 6 K: WIDE1
+//     12.8, WIDE2 14.5; 256 windowed trees of 2-12: WIDE1 37, WIDE2 39, NARROW2 40
+//   above, 24 trees of 16-32: WIDE4 174, WIDE2 205; one workgroup of eight wavefronts for 512 columns was 10-20%
+//     slower than two of WIDE4, whose barriers stop fewer wavefronts
+TreeForm tree_attn_form(int dtype, int head_dim, const void* k_pool, const void* v_pool, int cols, bool light) {
+  if (dtype != 1 || head_dim != 64 || ((uintptr_t)k_pool | (uintptr_t)v_pool) % 16) return {TREE_ANY, 16, 12};
+  if (cols <= 32) return {TREE_NARROW1, 32, 8};
+  if (cols <= 64 && !light) return {TREE_NARROW2, 64, 8};
+  if (cols <= 128) return light ? TreeForm{TREE_WIDE1, 128, 3} : TreeForm{TREE_WIDE2, 128, 4};
+  return {TREE_WIDE4, 256, 2};
 }
 
 hipError_t launch_tree_attn(int dtype, int head_dim, const TreeAttn& p, hipStream_t s) {
   if (p.n_items == 0) return hipSuccess;
-  // bf16 with head dim 64 takes the wide products, whose pages go to LDS by 16-byte direct loads: 16-byte
-  // aligned pools only. As many wavefronts as the largest tree has columns share a page.
-  if (dtype == 1 && head_dim == 64 && ((uintptr_t)p.k_pool | (uintptr_t)p.v_pool) % 16 == 0) {
-    const int cols = p.max_nodes * (p.hq / p.hkv);
-    if (cols <= 64) return tree_wide_impl<1, 4>(p, s);
-    if (cols <= 128) return tree_wide_impl<2, 6>(p, s);
-    if (cols <= 256) return tree_wide_impl<4, 6>(p, s);
-    return tree_wide_impl<8, 6>(p, s);
+  const int cols = p.max_nodes * (p.hq / p.hkv), tiles = (cols + p.form.cols - 1) / p.form.cols;
+  // groups in multiples of eight: one for each XCD
+  const int64_t groups = ((int64_t)p.n_items * p.hkv + 7) / 8 * 8 * tiles;
+  if (groups > 0x7FFFFFFF) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)groups);
+  switch (p.form.kind) {
+    case TREE_NARROW1: hipLaunchKernelGGL(tree_attn_narrow_kernel<1>, grid, dim3(64), 0, s, p, tiles); break;
+    case TREE_NARROW2: hipLaunchKernelGGL(tree_attn_narrow_kernel<2>, grid, dim3(64), 0, s, p, tiles); break;
+    case TREE_WIDE1: hipLaunchKernelGGL((tree_attn_wide_kernel<4, 1, 6>), grid, dim3(256), 0, s, p, tiles); break;
+    case TREE_WIDE2: hipLaunchKernelGGL((tree_attn_wide_kernel<2, 2, 4>), grid, dim3(128), 0, s, p, tiles); break;
+    case TREE_WIDE4: hipLaunchKernelGGL((tree_attn_wide_kernel<4, 2, 6>), grid, dim3(256), 0, s, p, tiles); break;
+    default: {
+      const dim3 fours((unsigned)((groups + 3) / 4)), block(256);
+      if (dtype == 0) {
+        if (head_dim == 32) hipLaunchKernelGGL((tree_attn_kernel<float, 32>), fours, block, 0, s, p, tiles);
+        else hipLaunchKernelGGL((tree_attn_kernel<float, 64>), fours, block, 0, s, p, tiles);
+      } else {
+        if (head_dim == 32) hipLaunchKernelGGL((tree_attn_kernel<bf16, 32>), fours, block, 0, s, p, tiles);
+        else hipLaunchKernelGGL((tree_attn_kernel<bf16, 64>), fours, block, 0, s, p, tiles);
+      }
+    }
   }
-  if (dtype == 0) return head_dim == 32 ? tree_attn_impl<float, 32>(p, s) : tree_attn_impl<float, 64>(p, s);
-  return head_dim == 32 ? tree_attn_impl<bf16, 32>(p, s) : tree_attn_impl<bf16, 64>(p, s);
+  return hipGetLastError();
 }
 
 // ---------------------------------------------------------------------------
@@ -733,22 +1063,38 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeCombine P) {
   const unsigned id = blockIdx.x * 4 + uniform(threadIdx.x >> 6), hq = P.hq;
   const int t = id / hq, h = id % hq;
   if (t >= P.n_tokens) return;
-  const int b = uniform(P.tok_seq[t]);
-  if (b < 0 || b >= P.batch) return;  // arrays that disagree with the plan (error bit set there)
-  const int2 sp = P.seq_split[b];
-  const int row0 = uniform(sp.x), splits = uniform(sp.y);
-  const int t0 = uniform(P.cu_q[b]), n = uniform(P.cu_q[b + 1]) - t0, node = t - t0;
-  if (splits <= 1 || node < 0 || node >= n || row0 < 0 || (int64_t)row0 + (int64_t)splits * n > P.n_rows) return;
+  const int4 tok = P.tok[t];
+  const int row0 = uniform(tok.x), n = uniform(tok.y), splits = uniform(tok.z);
+  // a stale record (device arrays that disagree with the plan) stays inside the partial rows
+  if (splits <= 1 || row0 < 0 || n <= 0 || n > TREE_MAX_NODES || (int64_t)row0 + (int64_t)(splits - 1) * n >= P.n_rows) return;
   float M = -INFINITY, L = 0.f;
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int k = sub; k < splits; k += RW) {
-    const int64_t row = (int64_t)(row0 + k * n + node) * P.hq + h;
-    const float2 ml = *reinterpret_cast<const float2*>(P.part_ml + 2 * row);
-    const float4 v = *reinterpret_cast<const float4*>(P.part_acc + row * D + dim);
-    const float Mn = fmaxf(M, ml.x), sub_m = Mn == -INFINITY ? 0.f : Mn;
-    const float r = __builtin_amdgcn_exp2f(M - sub_m), f = __builtin_amdgcn_exp2f(ml.x - sub_m);
-    L = L * r + ml.y * f;
-    a.x = a.x * r + v.x * f; a.y = a.y * r + v.y * f; a.z = a.z * r + v.z * f; a.w = a.w * r + v.w * f;
+  constexpr int U = 4;  // rows in flight per lane
+  for (int k0 = sub; k0 < splits; k0 += U * RW) {
+    float2 ml[U];
+    float4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {  // past the end: the last split again, with no weight
+      const int k = k0 + u * RW;
+      const int64_t row = (int64_t)(row0 + min(k, splits - 1) * n) * P.hq + h;
+      ml[u] = *reinterpret_cast<const float2*>(P.part_ml + 2 * row);
+      v[u] = *reinterpret_cast<const float4*>(P.part_acc + row * D + dim);
+      ml[u].x = k < splits ? ml[u].x : -INFINITY;
+    }
+    float Mn = M;
+#pragma unroll
+    for (int u = 0; u < U; ++u) Mn = fmaxf(Mn, ml[u].x);
+    const float base = Mn == -INFINITY ? 0.f : Mn, r = __builtin_amdgcn_exp2f(M - base);
+    L *= r;
+    a.x *= r; a.y *= r; a.z *= r; a.w *= r;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool in = k0 + u * RW < splits;  // a row that is not finite keeps its weight
+      const float f = in ? __builtin_amdgcn_exp2f(ml[u].x - base) : 0.f;
+      L += in ? ml[u].y * f : 0.f;
+      a.x += in ? v[u].x * f : 0.f; a.y += in ? v[u].y * f : 0.f;
+      a.z += in ? v[u].z * f : 0.f; a.w += in ? v[u].w * f : 0.f;
+    }
     M = Mn;
   }
   // join the lane groups, then the sink
