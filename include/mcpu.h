@@ -393,6 +393,19 @@ int decode_layer(const mcpu_layer_cfg* cfg, const mcpu_layer_weights* w, mcpu_kv
                  float* topk_w, const mcpu_taps* taps, void* workspace, size_t ws_bytes,
                  hipStream_t stream);
 
+/* decode_layer where the new tokens of each sequence are a tree of drafted tokens
+ * (above): the same step and arguments, with q and k rotated at the nodes'
+ * positions p_i and tree_attention over the pages. Cache positions seq_lens[b] ..
+ * seq_lens[b] + n - 1 receive the nodes' K and V; kv_tree_commit keeps the accepted
+ * ones. cu_q, host_cu_q and parents (device int32 [n_tokens]) are required; a node
+ * whose position lies beyond the RoPE table sets MCPU_DEVERR_ROPE. */
+size_t decode_layer_tree_workspace_size(const mcpu_layer_cfg* cfg, int32_t max_batch, int32_t max_tokens);
+int decode_layer_tree(const mcpu_layer_cfg* cfg, const mcpu_layer_weights* w, mcpu_kv_pool* pool, int32_t batch,
+                      const int32_t* page_table, int32_t max_pages, const int32_t* seq_lens, const int32_t* cu_q,
+                      const int32_t* parents, const int32_t* host_seq_lens, const int32_t* host_cu_q,
+                      const float* x_in, float* x_out, int32_t* topk_idx, float* topk_w, const mcpu_taps* taps,
+                      void* workspace, size_t ws_bytes, hipStream_t stream);
+
 /* decode_layer for callers that cannot allocate (code under HIP graph
  * capture, tight serving loops, harnesses that forbid allocation): the same
  * step, arguments and results as decode_layer, but its workspace is a static
@@ -500,7 +513,7 @@ enum {
   MCPU_KERNEL_KV_APPEND = 11,
   MCPU_KERNEL_ATTN_PREFILL = 12, /* chunked-prefill attention */
   MCPU_KERNEL_LM_HEAD = 13,      /* vocabulary projection + sampling summaries */
-  MCPU_KERNEL_TREE_PLAN = 14,
+  MCPU_KERNEL_TREE_PLAN = 14,    /* tree plan of large batches; node positions in decode_layer_tree */
   MCPU_KERNEL_TREE_ATTN = 15,    /* tree attention, a split each */
   MCPU_KERNEL_TREE_COMBINE = 16,
   MCPU_KERNEL_TREE_ACCEPT = 17,

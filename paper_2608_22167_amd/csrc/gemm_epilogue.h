@@ -127,12 +127,13 @@ __device__ __forceinline__ void qkv_store(const Gemm& P, int t, int head, int j0
   const int D = P.head_dim, half = D / 2;
   const int pos = P.tok_pos[t];
   if (head < P.hq + P.hkv) {  // q or k: rotate the pairs (j, j + d/2)
-    if (pos < 0 || pos >= P.rope_max_pos) {
+    const int at = P.tok_rope ? P.tok_rope[t] : pos;
+    if (at < 0 || at >= P.rope_max_pos) {
       set_error(P.err, 2);
       return;
     }
-    const float4* cp = reinterpret_cast<const float4*>(P.rope_cos + (int64_t)pos * half + j0);
-    const float4* sp = reinterpret_cast<const float4*>(P.rope_sin + (int64_t)pos * half + j0);
+    const float4* cp = reinterpret_cast<const float4*>(P.rope_cos + (int64_t)at * half + j0);
+    const float4* sp = reinterpret_cast<const float4*>(P.rope_sin + (int64_t)at * half + j0);
     const float4 ca = cp[0], cb = cp[1], sa = sp[0], sb = sp[1];
     const float cs[8] = {ca.x, ca.y, ca.z, ca.w, cb.x, cb.y, cb.z, cb.w};
     const float sn[8] = {sa.x, sa.y, sa.z, sa.w, sb.x, sb.y, sb.z, sb.w};

@@ -171,7 +171,8 @@ struct Gemm {
   const int32_t* page_table;
   int max_pages, n_pages;
   const int32_t* tok_seq;
-  const int32_t* tok_pos;
+  const int32_t* tok_pos;   // cache position of each row
+  const int32_t* tok_rope;  // position each row is rotated at, or nullptr: its cache position
   const float* rope_cos;
   const float* rope_sin;
   int rope_max_pos;

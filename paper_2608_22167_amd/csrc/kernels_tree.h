@@ -55,6 +55,9 @@ struct TreeAttn : TreeArgs {
 };
 hipError_t launch_tree_attn(int dtype, int head_dim, const TreeAttn& p, hipStream_t s);
 
+// rope[t] = len + depth of each node: the position its q and k are rotated at
+hipError_t launch_tree_positions(const TreeArgs& p, int32_t* rope, hipStream_t s);
+
 struct TreeCombine {
   const float* part_ml;
   const float* part_acc;

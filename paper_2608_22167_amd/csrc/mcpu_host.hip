@@ -459,7 +459,7 @@ constexpr int TREE_PPS_MIN = 12;       // pages per split at least (measured: 8 
 constexpr int TREE_START_PAGES = 32;   // what starting and ending a split costs, in pages
 
 struct TreePlanHost {
-  int n_tokens = 0, max_nodes = 0, max_pos = 0;
+  int n_tokens = 0, max_nodes = 0, max_len = 0;
   int pps = 1, n_items = 0, n_rows = 0;
   TreeForm form{};
 };
@@ -484,7 +484,7 @@ int plan_tree(const mcpu_layer_cfg* c, const mcpu_kv_pool* pool, int batch, int 
     if (n > 0 && ((long long)hsl[b] + n - 1) / PAGE_SIZE >= max_pages)
       return fail(MCPU_EINVAL, "sequence %d position %lld beyond page table width %d", b, (long long)hsl[b] + n - 1, max_pages);
     out->max_nodes = std::max(out->max_nodes, n);
-    if (n > 0) out->max_pos = std::max(out->max_pos, hsl[b] + n - 1);
+    if (n > 0) out->max_len = std::max(out->max_len, hsl[b]);
     longest = std::max(longest, pages_of(b, n));
     total += pages_of(b, n);
   }
@@ -553,14 +553,21 @@ TreeBufs carve_tree(Carve& cv, const mcpu_layer_cfg* c, int max_batch, int max_t
   return b;
 }
 
+TreeArgs tree_args(const mcpu_layer_cfg* c, int batch, int max_pages, const int32_t* seq_lens, const int32_t* cu_q,
+                   const int32_t* parents, const TreePlanHost& ph, int32_t* err) {
+  TreeArgs a{};
+  a.seq_lens = seq_lens; a.cu_q = cu_q; a.parents = parents; a.batch = batch; a.n_tokens = ph.n_tokens;
+  a.max_pages = max_pages; a.window = c->window; a.pps = ph.pps; a.n_items = ph.n_items; a.n_rows = ph.n_rows;
+  a.err = err;
+  return a;
+}
+
 int run_tree_attention(const mcpu_layer_cfg* c, const float* sinks, mcpu_kv_pool* pool, int batch,
                        const int32_t* page_table, int max_pages, const int32_t* seq_lens, const int32_t* cu_q,
                        const int32_t* parents, const TreePlanHost& ph, const void* q, void* o, const TreeBufs& tb,
                        int32_t* err, hipStream_t st) {
   TreeAttn ta{};
-  ta.seq_lens = seq_lens; ta.cu_q = cu_q; ta.parents = parents; ta.batch = batch; ta.n_tokens = ph.n_tokens;
-  ta.max_pages = max_pages; ta.window = c->window; ta.pps = ph.pps; ta.n_items = ph.n_items; ta.n_rows = ph.n_rows;
-  ta.err = err;
+  static_cast<TreeArgs&>(ta) = tree_args(c, batch, max_pages, seq_lens, cu_q, parents, ph, err);
   if (batch > TREE_SCAN && ph.n_rows > 0) {
     Timed tm(MCPU_KERNEL_TREE_PLAN, st);
     HIP_TRY(launch_tree_plan(ta, tb.item, st));
@@ -881,27 +888,66 @@ size_t layer_split_floats(const mcpu_layer_cfg* c, int max_rows) {
   return m;
 }
 
-size_t decode_layer_workspace_size(const mcpu_layer_cfg* cfg, int32_t max_batch, int32_t max_tokens) {
+// The buffers of one layer step: the plan (of split attention, or of trees) and the
+// intermediates.
+struct LayerBufs {
+  AttnBufs ab;
+  TreeBufs tb;
+  int32_t* tok_rope;
+  void *xn, *q, *o;
+  float* h1;
+  MoeBufs mb;
+  float* part;        // split partial tiles of the projections
+  int32_t* part_cnt;  // their arrival counters
+  size_t part_floats;
+};
+
+static LayerBufs carve_layer(Carve& cv, const mcpu_layer_cfg* c, int max_batch, int max_tokens, bool tree) {
+  const int T = std::max(max_tokens, max_batch);
+  const size_t db = dtype_bytes(c);
+  LayerBufs l{};
+  if (tree) {  // of the plan only the rows' sequences and cache positions
+    l.ab.tok_seq = cv.take<int32_t>(T);
+    l.ab.tok_pos = cv.take<int32_t>(T);
+    l.ab.split_start = cv.take<int32_t>(T + 1);
+    l.tok_rope = cv.take<int32_t>(T);
+    l.tb = carve_tree(cv, c, max_batch, T);
+  } else {
+    l.ab = carve_attention(cv, c, T);
+  }
+  l.xn = cv.take_bytes((size_t)T * c->hidden * db);
+  l.q = cv.take_bytes((size_t)T * c->n_q_heads * c->head_dim * db);
+  l.o = cv.take_bytes((size_t)T * c->n_q_heads * c->head_dim * db);
+  l.h1 = cv.take<float>((size_t)T * c->hidden);
+  l.mb = carve_moe(cv, c, T);
+  l.part_floats = layer_split_floats(c, T);
+  l.part = cv.take<float>(l.part_floats);
+  l.part_cnt = cv.take<int32_t>(SPLIT_MAX_TILES);
+  return l;
+}
+
+static size_t layer_workspace(const mcpu_layer_cfg* cfg, int32_t max_batch, int32_t max_tokens, bool tree) {
   if (check_cfg(cfg)) return 0;
-  int T = std::max(max_tokens, max_batch);
   Carve cv(nullptr);
-  carve_attention(cv, cfg, T);
-  size_t db = dtype_bytes(cfg);
-  cv.take_bytes((size_t)T * cfg->hidden * db);                        // xn
-  cv.take_bytes((size_t)T * cfg->n_q_heads * cfg->head_dim * db);     // q
-  cv.take_bytes((size_t)T * cfg->n_q_heads * cfg->head_dim * db);     // o
-  cv.take<float>((size_t)T * cfg->hidden);                            // h1
-  carve_moe(cv, cfg, T);
-  cv.take<float>(layer_split_floats(cfg, T));                         // split partial tiles
-  cv.take<int32_t>(SPLIT_MAX_TILES);                                  // their arrival counters
+  carve_layer(cv, cfg, max_batch, max_tokens, tree);
   return (cv.off + 255) & ~size_t(255);
 }
 
-int decode_layer(const mcpu_layer_cfg* cfg, const mcpu_layer_weights* w, mcpu_kv_pool* pool, int32_t batch,
-                 const int32_t* page_table, int32_t max_pages, const int32_t* seq_lens, const int32_t* cu_q,
-                 const int32_t* host_seq_lens, const int32_t* host_cu_q, const float* x_in, float* x_out,
-                 int32_t* topk_idx, float* topk_w, const mcpu_taps* taps, void* workspace, size_t ws_bytes,
-                 hipStream_t stream) {
+size_t decode_layer_workspace_size(const mcpu_layer_cfg* cfg, int32_t max_batch, int32_t max_tokens) {
+  return layer_workspace(cfg, max_batch, max_tokens, false);
+}
+
+size_t decode_layer_tree_workspace_size(const mcpu_layer_cfg* cfg, int32_t max_batch, int32_t max_tokens) {
+  if (max_batch < 0 || max_tokens < 0) return 0;
+  return layer_workspace(cfg, max_batch, max_tokens, true);
+}
+
+// One layer step; with `parents` the new tokens of each sequence are a tree.
+static int layer_step(const mcpu_layer_cfg* cfg, const mcpu_layer_weights* w, mcpu_kv_pool* pool, int32_t batch,
+                      const int32_t* page_table, int32_t max_pages, const int32_t* seq_lens, const int32_t* cu_q,
+                      const int32_t* parents, const int32_t* host_seq_lens, const int32_t* host_cu_q,
+                      const float* x_in, float* x_out, int32_t* topk_idx, float* topk_w, const mcpu_taps* taps,
+                      void* workspace, size_t ws_bytes, hipStream_t stream, bool tree) {
   int rc = check_cfg(cfg);
   if (rc) return rc;
   if ((rc = check_weights(cfg, w, true))) return rc;
@@ -909,83 +955,111 @@ int decode_layer(const mcpu_layer_cfg* cfg, const mcpu_layer_weights* w, mcpu_kv
   if (batch <= 0 || max_pages <= 0) return fail(MCPU_EINVAL, "batch %d, max_pages %d", batch, max_pages);
   if (!page_table || !seq_lens || !x_in || !x_out || !workspace) return fail(MCPU_EINVAL, "NULL pointer");
   if (x_in == x_out) return fail(MCPU_EINVAL, "x_in and x_out must not alias");
+  if (tree && (!cu_q || !parents)) return fail(MCPU_EINVAL, "cu_q or parents is NULL");
   if ((cu_q == nullptr) != (host_cu_q == nullptr)) return fail(MCPU_EINVAL, "cu_q and host_cu_q must both be given or both NULL");
   AttnPlanHost ph;
-  if ((rc = plan_attention(cfg, batch, max_pages, host_seq_lens, host_cu_q, &ph))) return rc;
+  TreePlanHost tp;
+  if (tree) {
+    if ((rc = plan_tree(cfg, pool, batch, max_pages, host_seq_lens, host_cu_q, &tp))) return rc;
+    ph.n_tokens = tp.n_tokens;
+    ph.max_pos = tp.max_len;  // a root's position; nodes further on are checked on the device
+    ph.prefill_min_q = 1;     // no token takes split attention
+  } else if ((rc = plan_attention(cfg, batch, max_pages, host_seq_lens, host_cu_q, &ph))) {
+    return rc;
+  }
   const int T = ph.n_tokens;
   if (T == 0) return MCPU_OK;
   if (ph.max_pos >= w->rope_max_pos)
     return fail(MCPU_EINVAL, "position %d beyond the RoPE table (%d rows)", ph.max_pos, w->rope_max_pos);
-  size_t need = decode_layer_workspace_size(cfg, batch, T);
+  size_t need = layer_workspace(cfg, batch, T, tree);
   if (ws_bytes < need) return fail(MCPU_ENOMEM, "workspace %zu bytes < %zu needed", ws_bytes, need);
 
   const int H = cfg->hidden, D = cfg->head_dim, Hq = cfg->n_q_heads, Hkv = cfg->n_kv_heads;
   const size_t db = dtype_bytes(cfg);
   Carve cv(workspace);
-  const int Tc = std::max(T, batch);
-  AttnBufs ab = carve_attention(cv, cfg, Tc);
-  void* xn = cv.take_bytes((size_t)Tc * H * db);
-  void* q = cv.take_bytes((size_t)Tc * Hq * D * db);
-  void* o = cv.take_bytes((size_t)Tc * Hq * D * db);
-  float* h1 = cv.take<float>((size_t)Tc * H);
-  MoeBufs mb = carve_moe(cv, cfg, Tc);
-  const size_t split_floats = layer_split_floats(cfg, Tc);
-  float* part = cv.take<float>(split_floats);
-  int32_t* part_cnt = cv.take<int32_t>(SPLIT_MAX_TILES);
+  const LayerBufs l = carve_layer(cv, cfg, batch, T, tree);
+  const AttnBufs& ab = l.ab;
   int32_t* err = err_word(workspace);
 
   // the plan and RMSNorm_1 share one launch (the norm does not depend on it)
   RmsNorm rn{};
-  rn.x = x_in; rn.g = w->g1; rn.n_tokens = T; rn.hidden = H; rn.eps = cfg->rms_eps; rn.out = xn;
+  rn.x = x_in; rn.g = w->g1; rn.n_tokens = T; rn.hidden = H; rn.eps = cfg->rms_eps; rn.out = l.xn;
   {
     Timed tm(MCPU_KERNEL_ATTN_PLAN, stream);
     AttnPlan pl = make_plan(cfg, batch, seq_lens, cu_q, ph, ab, err);
-    if (split_floats) {  // the split GEMMs' counters start at zero
-      pl.zero = part_cnt;
+    if (l.part_floats) {  // the split GEMMs' counters start at zero
+      pl.zero = l.part_cnt;
       pl.n_zero = SPLIT_MAX_TILES;
     }
     pl.norm = rn;
     pl.norm_dtype = cfg->dtype;
     HIP_TRY(launch_attn_plan(pl, stream));
   }
+  if (tree) {
+    Timed tm(MCPU_KERNEL_TREE_PLAN, stream);
+    HIP_TRY(launch_tree_positions(tree_args(cfg, batch, max_pages, seq_lens, cu_q, parents, tp, err), l.tok_rope, stream));
+  }
 
   Gemm gq{};
-  gq.w = w->w_qkv; gq.n = (Hq + 2 * Hkv) * D; gq.k = H; gq.x = xn; gq.n_rows = T; gq.n_groups = 1;
-  gq.epi = EPI_QKV; gq.bias = w->b_qkv; gq.hq = Hq; gq.hkv = Hkv; gq.head_dim = D; gq.q_out = q;
+  gq.w = w->w_qkv; gq.n = (Hq + 2 * Hkv) * D; gq.k = H; gq.x = l.xn; gq.n_rows = T; gq.n_groups = 1;
+  gq.epi = EPI_QKV; gq.bias = w->b_qkv; gq.hq = Hq; gq.hkv = Hkv; gq.head_dim = D; gq.q_out = l.q;
   gq.k_pool = pool->k; gq.v_pool = pool->v; gq.page_table = page_table; gq.max_pages = max_pages;
-  gq.n_pages = pool->n_pages; gq.tok_seq = ab.tok_seq; gq.tok_pos = ab.tok_pos; gq.rope_cos = w->rope_cos;
+  gq.n_pages = pool->n_pages; gq.tok_seq = ab.tok_seq; gq.tok_pos = ab.tok_pos; gq.tok_rope = l.tok_rope;
+  gq.rope_cos = w->rope_cos;
   gq.rope_sin = w->rope_sin; gq.rope_max_pos = w->rope_max_pos; gq.err = err; gq.max_rows_per_group = T;
   gq.w_packed = cfg->dtype == MCPU_BF16 ? w->w_qkv_packed : nullptr;
-  if (split_floats) { gq.part = part; gq.part_cnt = part_cnt; }
+  if (l.part_floats) { gq.part = l.part; gq.part_cnt = l.part_cnt; }
   {
     Timed tm(MCPU_KERNEL_QKV, stream);
     HIP_TRY(launch_gemm(cfg->dtype, MCPU_EXPERT_DENSE, gq, stream));
   }
 
-  if ((rc = run_attention(cfg, w->sinks, pool, batch, page_table, max_pages, seq_lens, cu_q, ph, q, o, ab, err,
-                          stream, true)))
-    return rc;
+  if (tree)
+    rc = run_tree_attention(cfg, w->sinks, pool, batch, page_table, max_pages, seq_lens, cu_q, parents, tp, l.q, l.o,
+                            l.tb, err, stream);
+  else
+    rc = run_attention(cfg, w->sinks, pool, batch, page_table, max_pages, seq_lens, cu_q, ph, l.q, l.o, ab, err, stream,
+                       true);
+  if (rc) return rc;
 
   Gemm go{};
-  go.w = w->w_o; go.n = H; go.k = Hq * D; go.x = o; go.n_rows = T; go.n_groups = 1; go.epi = EPI_RESIDUAL;
-  go.bias = w->b_o; go.residual = x_in; go.out = h1; go.err = err; go.max_rows_per_group = T;
+  go.w = w->w_o; go.n = H; go.k = Hq * D; go.x = l.o; go.n_rows = T; go.n_groups = 1; go.epi = EPI_RESIDUAL;
+  go.bias = w->b_o; go.residual = x_in; go.out = l.h1; go.err = err; go.max_rows_per_group = T;
   go.w_packed = cfg->dtype == MCPU_BF16 ? w->w_o_packed : nullptr;
-  if (split_floats) { go.part = part; go.part_cnt = part_cnt; }
+  if (l.part_floats) { go.part = l.part; go.part_cnt = l.part_cnt; }
   {
     Timed tm(MCPU_KERNEL_OPROJ, stream);
     HIP_TRY(launch_gemm(cfg->dtype, MCPU_EXPERT_DENSE, go, stream));
   }
 
-  if ((rc = run_moe(cfg, w, T, h1, x_out, topk_idx, topk_w, nullptr, mb, err, stream,
+  if ((rc = run_moe(cfg, w, T, l.h1, x_out, topk_idx, topk_w, nullptr, l.mb, err, stream,
                     taps ? taps->logits : nullptr)))
     return rc;
 
   if (taps) {
-    if (taps->q) HIP_TRY(hipMemcpyAsync(taps->q, q, (size_t)T * Hq * D * db, hipMemcpyDeviceToDevice, stream));
-    if (taps->o) HIP_TRY(hipMemcpyAsync(taps->o, o, (size_t)T * Hq * D * db, hipMemcpyDeviceToDevice, stream));
-    if (taps->h1) HIP_TRY(hipMemcpyAsync(taps->h1, h1, (size_t)T * H * 4, hipMemcpyDeviceToDevice, stream));
+    if (taps->q) HIP_TRY(hipMemcpyAsync(taps->q, l.q, (size_t)T * Hq * D * db, hipMemcpyDeviceToDevice, stream));
+    if (taps->o) HIP_TRY(hipMemcpyAsync(taps->o, l.o, (size_t)T * Hq * D * db, hipMemcpyDeviceToDevice, stream));
+    if (taps->h1) HIP_TRY(hipMemcpyAsync(taps->h1, l.h1, (size_t)T * H * 4, hipMemcpyDeviceToDevice, stream));
   }
   return MCPU_OK;
+}
+
+int decode_layer(const mcpu_layer_cfg* cfg, const mcpu_layer_weights* w, mcpu_kv_pool* pool, int32_t batch,
+                 const int32_t* page_table, int32_t max_pages, const int32_t* seq_lens, const int32_t* cu_q,
+                 const int32_t* host_seq_lens, const int32_t* host_cu_q, const float* x_in, float* x_out,
+                 int32_t* topk_idx, float* topk_w, const mcpu_taps* taps, void* workspace, size_t ws_bytes,
+                 hipStream_t stream) {
+  return layer_step(cfg, w, pool, batch, page_table, max_pages, seq_lens, cu_q, nullptr, host_seq_lens, host_cu_q, x_in,
+                    x_out, topk_idx, topk_w, taps, workspace, ws_bytes, stream, false);
+}
+
+int decode_layer_tree(const mcpu_layer_cfg* cfg, const mcpu_layer_weights* w, mcpu_kv_pool* pool, int32_t batch,
+                      const int32_t* page_table, int32_t max_pages, const int32_t* seq_lens, const int32_t* cu_q,
+                      const int32_t* parents, const int32_t* host_seq_lens, const int32_t* host_cu_q,
+                      const float* x_in, float* x_out, int32_t* topk_idx, float* topk_w, const mcpu_taps* taps,
+                      void* workspace, size_t ws_bytes, hipStream_t stream) {
+  return layer_step(cfg, w, pool, batch, page_table, max_pages, seq_lens, cu_q, parents, host_seq_lens, host_cu_q, x_in,
+                    x_out, topk_idx, topk_w, taps, workspace, ws_bytes, stream, true);
 }
 
 size_t lm_head_workspace_size(int32_t hidden, int32_t vocab, int32_t max_tokens) {

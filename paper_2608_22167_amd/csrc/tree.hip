@@ -203,6 +203,24 @@ __device__ __forceinline__ Nodes nodes_of(const TreeArgs& P, const TreeItem& it)
   return d;
 }
 
+// The positions at which a layer rotates its nodes, a wavefront per tree. Bound by
+// latency (3 us).
+__global__ __launch_bounds__(256) void tree_positions_kernel(TreeArgs P, int32_t* rope) {
+  const int b = blockIdx.x * 4 + uniform(threadIdx.x >> 6), lane = lane_id();
+  if (b >= P.batch) return;
+  const TreeSpan s = tree_span(P, b, true);
+  TreeItem it{};
+  it.t0 = uniform(s.t0);
+  it.n = uniform(s.n);
+  const Nodes d = nodes_of(P, it);
+  if (lane < it.n) rope[it.t0 + lane] = s.len + d.depth;
+}
+
+hipError_t launch_tree_positions(const TreeArgs& p, int32_t* rope, hipStream_t s) {
+  hipLaunchKernelGGL(tree_positions_kernel, dim3((p.batch + 3) / 4), dim3(256), 0, s, p, rope);
+  return hipGetLastError();
+}
+
 // What the combine needs to know of a tree's tokens: the first partial row, the
 // rows from one split to the next, and the splits. Written by one wavefront of the
 // tree's first split, in steps that have a combine.

@@ -18,11 +18,20 @@ pages of sliding-window layers are freed once they fall wholly left of the
 window, and all of a sequence's pages are freed when it is released.
 `score()` recomputes the log-probabilities of whole trajectories (the GRPO
 update's log-prob pass): a long causal prefill with targets, no sampling.
+
+`add_group()` starts the members of a group (the policy update compares several
+trajectories of one prompt) on pages that they share: the prompt is prefilled
+once, `fork()` gives every member the whole pages and a copy of the last, partly
+filled one. `step_tree()` verifies drafted tokens: where a drafted token equals the
+draw before it, the step yields more than one token per sequence, and because a
+draw depends only on (seed, sequence, position) they are the tokens that `step()`
+would have drawn one by one. `Lookup` drafts from the sequence's own history.
 """
 from __future__ import annotations
 
+from collections import deque
 from dataclasses import dataclass, field
-from typing import Dict, List, Optional, Sequence
+from typing import Dict, List, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
@@ -65,6 +74,50 @@ class _Seq:
     history: List[int] = field(default_factory=list)    # every token fed so far
 
 
+class Lookup:
+    """Drafts from one sequence's own tokens: what followed the latest places at
+    which its last tokens stood before (the last `ngram`, of fewer where there is
+    no such place). Tool observations and the model's quotes of them repeat."""
+
+    def __init__(self, ngram: int = 3, width: int = 2):
+        self.ngram, self.width = ngram, width
+        self.after: Dict[tuple, deque] = {}   # tokens -> the latest positions behind them
+        self.seen = 0
+
+    def tree(self, history: Sequence[int], max_nodes: int, max_depth: int) -> Tuple[List[int], List[int]]:
+        """At most max_nodes tokens, max_depth in a row, to follow `history` (a
+        longer one than at the last call, with the same beginning); the places'
+        common beginnings are shared. Returns the tokens and their parents (index of
+        the token before, -1: the history's end)."""
+        for i in range(max(self.seen, 1), len(history)):
+            for n in range(1, min(self.ngram, i) + 1):
+                self.after.setdefault(tuple(history[i - n:i]), deque(maxlen=self.width)).append(i)
+        self.seen = len(history)
+        places: Sequence[int] = ()
+        for n in range(min(self.ngram, len(history)), 0, -1):
+            places = self.after.get(tuple(history[-n:]), ())
+            if places:
+                break
+        runs = [history[p:p + max_depth] for p in reversed(places)]
+        tokens: List[int] = []
+        parents: List[int] = []
+        child: Dict[Tuple[int, int], int] = {}
+        ends = [-1] * len(runs)
+        for d in range(max_depth):        # level by level, so that a cut at max_nodes keeps every branch
+            for r, run in enumerate(runs):
+                if d >= len(run) or (d and ends[r] < 0):
+                    continue
+                key = (ends[r], run[d])
+                if key not in child:
+                    if len(tokens) >= max_nodes:
+                        return tokens, parents
+                    child[key] = len(tokens)
+                    tokens.append(run[d])
+                    parents.append(ends[r])
+                ends[r] = child[key]
+        return tokens, parents
+
+
 class Generator:
     """The stack's weights, one K/V pool pair per layer, the embedding and the
     vocabulary head, all resident on the GPU; sequences come and go."""
@@ -85,6 +138,7 @@ class Generator:
         self.alloc_full = self.pools[1] if spec.n_layers > 1 else None
         self.alloc_sw = self.pools[0]
         lm = W.lm_weights_device(spec.seed, ss.shape_full.hidden, spec.vocab, device)
+        self.tree_ws = None  # workspace of step_tree, made at its first call
         self.embed = lm["embed"]
         self.head = mcpu.DeviceLmHead(lm["g_final"], lm["w_lm"], ss.shape_full.rms_eps, device)
         self.max_tokens = max_tokens_per_step
@@ -115,6 +169,75 @@ class Generator:
             mcpu.kv_pages_free(self.alloc_full, np.array(s.pages_full, np.int32))
         if s.pages_sw:
             mcpu.kv_pages_free(self.alloc_sw, np.array(list(s.pages_sw.values()), np.int32))
+
+    def fork(self, sid: int, new_sids: Sequence[int]) -> None:
+        """Start each of new_sids as a copy of sequence sid (cache, history and
+        pending input): whole pages get another holder, a partly filled last
+        page is copied for each. All or nothing: MCPU_ENOMEM leaves every
+        sequence as it was."""
+        s, n = self.seqs[sid], len(new_sids)
+        if len(set(new_sids)) != n or any(k in self.seqs for k in new_sids):
+            raise ValueError(f"fork: sequence ids {list(new_sids)} repeat or exist")
+        if n == 0:
+            return
+        whole, part = s.length // PAGE, s.length % PAGE > 0
+        kinds = []  # (allocator, layer pools, shared pages, last page, its copies)
+        for alloc, pools, shared, last in (
+                (self.alloc_full, self.pools[1::2], s.pages_full[:whole], s.pages_full[whole:whole + 1]),
+                (self.alloc_sw, self.pools[0::2], [p for lp, p in s.pages_sw.items() if lp < whole],
+                 [p for lp, p in s.pages_sw.items() if lp == whole])):
+            if alloc is not None:
+                kinds.append((alloc, pools, shared, last if part else []))
+        copies: List[np.ndarray] = []
+        try:
+            for alloc, _, _, last in kinds:
+                copies.append(mcpu.kv_pages_alloc(alloc, n * len(last)))
+        except mcpu.McpuError:
+            for (alloc, _, _, _), ids in zip(kinds, copies):
+                mcpu.kv_pages_free(alloc, ids)
+            raise
+        for (alloc, pools, shared, last), ids in zip(kinds, copies):
+            mcpu.kv_pages_share(alloc, np.array(shared * n, np.int32))
+            if last:
+                src = np.full(n, last[0], np.int32)
+                d_src, d_dst = (torch.from_numpy(np.ascontiguousarray(a, np.int32)).to(self.device) for a in (src, ids))
+                for i in range(0, len(pools), mcpu.MAX_POOLS):
+                    mcpu.kv_pages_copy(pools[i:i + mcpu.MAX_POOLS], d_src, d_dst, src, ids, self.ws)
+        full = copies[0] if self.alloc_full is not None else np.zeros(0, np.int32)
+        for j, k in enumerate(new_sids):
+            c = _Seq(k, s.length, list(s.pending), s.pages_full[:whole], {}, list(s.history))
+            if part and self.alloc_full is not None:
+                c.pages_full.append(int(full[j]))
+            c.pages_sw = {lp: p for lp, p in s.pages_sw.items() if lp < whole}
+            if part and len(copies[-1]):
+                c.pages_sw[whole] = int(copies[-1][j])
+            self.seqs[k] = c
+            if sid in self.held:
+                self.held[k] = list(self.held[sid])
+
+    def add_group(self, sids: Sequence[int], tokens: Sequence[int]) -> None:
+        """Start the sequences sids on one prompt: its tokens but the last are
+        prefilled once and shared, the last is each member's pending input, so
+        that every member draws its own next token."""
+        tokens = [int(t) for t in tokens]
+        if not len(sids) or not tokens:
+            raise ValueError("add_group needs sequence ids and a prompt")
+        if len(set(sids)) != len(sids) or any(k in self.seqs for k in sids):
+            raise ValueError(f"add_group: sequence ids {list(sids)} repeat or exist")
+        s = self.seqs[sids[0]] = _Seq(sids[0], pending=tokens)
+        try:
+            while len(s.pending) > 1:
+                q = min(len(s.pending) - 1, self.max_tokens)
+                self._grow(s, q)
+                self._forward([s], [q], np.array(s.pending[:q], np.int64))
+                s.history.extend(s.pending[:q])
+                del s.pending[:q]
+                s.length += q
+                self._shrink(s)
+            self.fork(sids[0], sids[1:])
+        except mcpu.McpuError:
+            self.release(sids[0])
+            raise
 
     def free_pages(self):
         return (self.alloc_full.free_pages() if self.alloc_full is not None else 0, self.alloc_sw.free_pages())
@@ -147,14 +270,18 @@ class Generator:
         pt_f = -np.ones((len(batch), max_lp), np.int32)
         pt_s = -np.ones((len(batch), max_lp), np.int32)
         for b, s in enumerate(batch):
-            pt_f[b, :len(s.pages_full)] = s.pages_full
+            own = s.pages_full[:max_lp]  # a tree step may have left pages behind the last position
+            pt_f[b, :len(own)] = own
             for lp, p in s.pages_sw.items():
-                pt_s[b, lp] = p
+                if lp < max_lp:
+                    pt_s[b, lp] = p
         return pt_f, pt_s
 
-    def _forward(self, batch: List[_Seq], q_lens: List[int], tokens: np.ndarray):
+    def _forward(self, batch: List[_Seq], q_lens: List[int], tokens: np.ndarray, parents: Optional[np.ndarray] = None):
         """Embeds the step's input tokens and runs every layer; returns the
-        final residual rows [T, H] and cu_q."""
+        final residual rows [T, H] and cu_q. With parents, the input of each
+        sequence is a tree of tokens, whose accepted path is still to be kept
+        (the device arrays for that are returned too)."""
         T = int(sum(q_lens))
         dev = self.device
         cu = np.zeros(len(batch) + 1, np.int32)
@@ -168,11 +295,17 @@ class Generator:
         H = self.ss.shape_full.hidden
         x = [torch.empty((T, H), device=dev), torch.empty((T, H), device=dev)]
         mcpu.embed_tokens(self.embed, d_tok, x[0], self.ws)
+        d_par = None if parents is None else torch.from_numpy(parents).to(dev)
         for i in range(self.spec.n_layers):
-            sw = self.ss.is_sw(i)
-            mcpu.decode_layer(self.ss.shape(i), self.weights[i], self.pools[i], d_pts if sw else d_ptf, d_sl, d_cu,
-                              seq_lens, cu, x[i % 2], x[(i + 1) % 2], workspace=self.ws)
-        return x[self.spec.n_layers % 2], cu
+            table = d_pts if self.ss.is_sw(i) else d_ptf
+            if parents is None:
+                mcpu.decode_layer(self.ss.shape(i), self.weights[i], self.pools[i], table, d_sl, d_cu, seq_lens, cu,
+                                  x[i % 2], x[(i + 1) % 2], workspace=self.ws)
+            else:
+                mcpu.decode_layer_tree(self.ss.shape(i), self.weights[i], self.pools[i], table, d_sl, d_cu, d_par,
+                                       seq_lens, cu, x[i % 2], x[(i + 1) % 2], workspace=self.tree_ws)
+        out = x[self.spec.n_layers % 2]
+        return (out, cu) if parents is None else (out, cu, dict(tok=d_tok, par=d_par, sl=d_sl, cu=d_cu, ptf=d_ptf, pts=d_pts))
 
     def step(self) -> Dict[int, tuple]:
         """Advance every sequence with pending input by up to its whole input
@@ -221,6 +354,70 @@ class Generator:
         self.steps += 1
         return out
 
+    def step_tree(self, drafts: Dict[int, Tuple[Sequence[int], Sequence[int]]]) -> Dict[int, List[tuple]]:
+        """Advance every decoding sequence (one pending token) with a tree of
+        drafted tokens behind it: drafts[sid] = (tokens, parents), parents being
+        indices into tokens or -1 for the pending token; at most
+        TREE_MAX_NODES - 1 of them, none for a sequence without a draft.
+        Returns {sid: [(token, logprob), ...]}: the draws along the confirmed
+        path, one at least, of which the last becomes the pending token. They
+        are the tokens that calls of `step()` would have drawn. Sequences with
+        longer input are left to `step()`; no more rows are fed than
+        max_tokens_per_step, oldest sequences first and drafts only where every
+        sequence has its row."""
+        ready = [s for s in self.seqs.values() if len(s.pending) == 1][:self.max_tokens]
+        batch, q_lens, toks, pars, depth, budget = [], [], [], [], [], self.max_tokens - len(ready)
+        for s in ready:
+            d_tok, d_par = drafts.get(s.sid, ((), ()))
+            if len(d_tok) != len(d_par) or len(d_tok) >= mcpu.TREE_MAX_NODES:
+                raise ValueError(f"draft of sequence {s.sid}: {len(d_tok)} tokens, {len(d_par)} parents")
+            dep = [0]
+            for i, p in enumerate(d_par):
+                if not -1 <= p < i:
+                    raise ValueError(f"draft of sequence {s.sid}: parent {p} of token {i}")
+                dep.append(dep[p + 1] + 1)
+            if len(d_tok) > budget:
+                d_tok, d_par, dep = (), (), [0]
+            budget -= len(d_tok)
+            batch.append(s)
+            q_lens.append(1 + len(d_tok))
+            toks += [s.pending[0], *(int(t) for t in d_tok)]
+            pars += [-1, *(int(p) + 1 for p in d_par)]
+            depth += dep
+        if not batch:
+            return {}
+        if self.tree_ws is None:
+            self.tree_ws = mcpu.workspace(max(mcpu.decode_layer_tree_workspace_size(self.ss.shape(i), self.max_tokens,
+                                                                                    self.max_tokens)
+                                              for i in range(min(2, self.spec.n_layers))), self.device)
+        for s, q in zip(batch, q_lens):
+            self._grow(s, q)
+        x, cu, d = self._forward(batch, q_lens, np.array(toks, np.int64), np.array(pars, np.int32))
+        dev, T, B = self.device, len(toks), len(batch)
+        up = lambda a: torch.from_numpy(np.array(a, np.int32)).to(dev)  # noqa: E731
+        lens = np.repeat([s.length for s in batch], q_lens)
+        sampled = torch.empty(T, dtype=torch.int32, device=dev)
+        lp = torch.empty(T, device=dev)
+        mcpu.lm_head_sample(self.head, x, self.spec.temperature, self.spec.seed,
+                            up(np.repeat([s.sid for s in batch], q_lens)), up(lens + np.array(depth) + 1), None, sampled,
+                            lp, workspace=self.lm_ws)
+        path, n_path, following = (torch.empty(n, dtype=torch.int32, device=dev) for n in (T, B, B))
+        mcpu.tree_accept(d["cu"], d["par"], d["tok"], sampled, path, n_path, following, self.tree_ws)
+        for pools, table in ((self.pools[0::2], d["pts"]), (self.pools[1::2], d["ptf"])):
+            for i in range(0, len(pools), mcpu.MAX_POOLS):
+                mcpu.kv_tree_commit(pools[i:i + mcpu.MAX_POOLS], table, d["sl"], d["cu"], path, n_path, self.tree_ws)
+        path, n_path, sampled, lp = path.cpu().numpy(), n_path.cpu().numpy(), sampled.cpu().numpy(), lp.cpu().numpy()
+        out = {}
+        for b, s in enumerate(batch):
+            rows = cu[b] + path[cu[b]:cu[b] + n_path[b]]
+            out[s.sid] = [(int(sampled[r]), float(lp[r])) for r in rows]
+            s.history.extend(int(toks[r]) for r in rows)
+            s.length += len(rows)
+            s.pending = [int(sampled[rows[-1]])]
+            self._shrink(s)
+        self.steps += 1
+        return out
+
     def hold(self, sid: int) -> None:
         """Drop the sequence's pending sampled token (its turn ended); the
         token is still part of the trajectory: it is fed with the next input."""
@@ -234,7 +431,8 @@ class Generator:
         self.add(sid, list(held) + list(observation))
 
     def check_errors(self) -> int:
-        return mcpu.mcpu_check_device_errors(self.ws) | mcpu.mcpu_check_device_errors(self.lm_ws)
+        bits = mcpu.mcpu_check_device_errors(self.ws) | mcpu.mcpu_check_device_errors(self.lm_ws)
+        return bits | (mcpu.mcpu_check_device_errors(self.tree_ws) if self.tree_ws is not None else 0)
 
     # ------------------------------------------------------------------ trajectory scoring
 

@@ -31,7 +31,7 @@ EXPORTED = ("mcpu_last_error", "kv_pool_create", "kv_pool_destroy", "kv_pool_fre
             "lm_head_workspace_size", "lm_head_sample", "embed_tokens", "decode_layer_noalloc",
             "mcpu_mxfp8_quantize", "mcpu_packed_mxfp4_bytes", "mcpu_pack_mxfp4",
             "kv_pages_share", "kv_page_holders", "kv_pages_copy", "tree_attention_workspace_size", "tree_attention",
-            "tree_accept", "kv_tree_commit")
+            "tree_accept", "kv_tree_commit", "decode_layer_tree_workspace_size", "decode_layer_tree")
 NOALLOC_SCRATCH_BYTES = 128 << 20  # the static scratch of decode_layer_noalloc, per GPU
 
 KERNELS = ("attn_plan", "rmsnorm", "qkv", "attn_split", "attn_combine", "oproj", "router", "permute",
@@ -100,6 +100,9 @@ def lib():
         L.decode_layer_workspace_size.restype = sz
         L.decode_layer.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                    vp, sz, vp]
+        L.decode_layer_tree_workspace_size.argtypes = [vp, i32, i32]
+        L.decode_layer_tree_workspace_size.restype = sz
+        L.decode_layer_tree.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.decode_layer_noalloc.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
         L.mcpu_check_device_errors.argtypes = [vp, vp, i32p]
         L.mcpu_packed_weights_bytes.argtypes = [i32, i32, i32]
@@ -392,6 +395,25 @@ def decode_layer(shape, weights: DeviceWeights, pool: KVPool, page_table, seq_le
                               _ptr(topk_idx), _ptr(topk_w),
                               ctypes.byref(taps) if taps is not None else None,
                               _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+def decode_layer_tree_workspace_size(shape, max_batch, max_tokens) -> int:
+    cfg = make_cfg(shape)
+    return lib().decode_layer_tree_workspace_size(ctypes.byref(cfg), max_batch, max_tokens)
+
+
+def decode_layer_tree(shape, weights: DeviceWeights, pool: KVPool, page_table, seq_lens, cu_q, parents, host_seq_lens,
+                      host_cu_q, x_in, x_out, topk_idx=None, topk_w=None, taps: Optional[Taps] = None,
+                      workspace=None, stream=None):
+    """decode_layer where each sequence's new tokens are a tree of drafted tokens."""
+    cfg = make_cfg(shape)
+    hs, hc = _host_i32(host_seq_lens), _host_i32(host_cu_q)
+    _check(lib().decode_layer_tree(ctypes.byref(cfg), ctypes.byref(weights.struct), pool.handle,
+                                   int(seq_lens.shape[0]), _ptr(page_table), int(page_table.shape[1]),
+                                   _ptr(seq_lens), _ptr(cu_q), _ptr(parents), _ptr(hs), _ptr(hc), _ptr(x_in),
+                                   _ptr(x_out), _ptr(topk_idx), _ptr(topk_w),
+                                   ctypes.byref(taps) if taps is not None else None,
+                                   _ptr(workspace), workspace.numel(), _stream(stream)))
 
 
 def decode_layer_noalloc(shape, weights: DeviceWeights, pool: KVPool, page_table, seq_lens, cu_q, host_seq_lens,

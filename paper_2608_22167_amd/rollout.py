@@ -34,6 +34,8 @@ from typing import Dict, List, Optional
 
 import numpy as np
 
+from paper_2608_22167_amd.generate import Lookup
+
 
 @dataclass
 class RolloutConfig:
@@ -74,10 +76,15 @@ class Engine:
     with pending input; `generate` (from any thread) feeds a sequence its
     input and returns a future of the next n sampled tokens (with their
     log-probabilities). A sampled token that ends a request is held back and
-    fed before the sequence's next input, so turns join seamlessly."""
+    fed before the sequence's next input, so turns join seamlessly. With
+    draft_nodes > 0, steps in which every sequence decodes verify that many tokens
+    drafted from each sequence's own history (`Generator.step_tree`): the same
+    tokens in fewer steps."""
 
-    def __init__(self, gen):
+    def __init__(self, gen, draft_nodes: int = 0):
         self.gen = gen
+        self.draft_nodes = draft_nodes
+        self.lookups: Dict[int, Lookup] = {}
         self.inbox: "queue.Queue" = queue.Queue()
         self.want: Dict[int, list] = {}
         self.busy_s = 0.0
@@ -116,7 +123,20 @@ class Engine:
             self.want[sid] = [n, [], f]
         elif kind == "release":
             self.gen.release(sid)
+            self.lookups.pop(sid, None)
             f.set_result(None)
+
+    def _step(self) -> Dict[int, list]:
+        """One step of the generator: {sid: [(token, logprob), ...]}."""
+        live = [s for s in self.gen.seqs.values() if s.pending] if self.draft_nodes else []
+        if not live or any(len(s.pending) > 1 for s in live):
+            return {sid: [o] for sid, o in self.gen.step().items()}
+        drafts = {}
+        for s in live:
+            left = self.want[s.sid][0] - len(self.want[s.sid][1]) if s.sid in self.want else 1
+            look = self.lookups.setdefault(s.sid, Lookup())
+            drafts[s.sid] = look.tree(s.history + s.pending, self.draft_nodes, left - 1)
+        return self.gen.step_tree(drafts)
 
     def _loop(self):
         try:
@@ -138,16 +158,16 @@ class Engine:
                 if not self.want:
                     continue
                 t0 = time.perf_counter()
-                out = self.gen.step()
+                out = self._step()
                 self.busy_s += time.perf_counter() - t0
                 self.steps += 1
                 self.batch_hist.append(len(out))
-                for sid, (tok, lp) in out.items():
+                for sid, drawn in out.items():
                     w = self.want.get(sid)
                     if w is None:
                         continue
-                    w[1].append((tok, lp))
-                    self.tokens += 1
+                    w[1].extend(drawn)
+                    self.tokens += len(drawn)
                     if len(w[1]) == w[0]:
                         self.gen.hold(sid)
                         del self.want[sid]

@@ -170,3 +170,102 @@ def test_reference_of_a_small_tree():
                                                  [0, 0, 0, 1, 0, 1]], bool))
     path, n, following = R.accept(_i32(0, 4), _i32(-1, 0, 0, 2), _i32(9, 5, 6, 7), _i32(6, 1, 7, 3))
     assert path.tolist() == [0, 2, 3, -1] and n.tolist() == [3] and following.tolist() == [3]
+
+
+# ------------------------------------------------------------------------------ drafting and the engine
+
+
+def test_lookup_drafts_from_earlier_places():
+    from paper_2608_22167_amd.generate import Lookup
+    look = Lookup(ngram=2, width=2)
+    h = [1, 2, 3, 4, 1, 2, 3, 5, 9, 1, 2]
+    # behind (1, 2): 3 5 .. (latest) and 3 4 ..: the 3 is shared
+    assert look.tree(h, 10, 2) == ([3, 5, 4], [-1, 0, 0])
+    assert look.tree(h, 2, 2) == ([3, 5], [-1, 0])
+    assert look.tree(h, 10, 0) == ([], []) and look.tree(h, 0, 5) == ([], [])
+    assert look.tree(h + [7], 10, 3) == ([], [])          # 7 never stood anywhere before
+    assert look.tree(h + [7, 3], 4, 2) == ([5, 4, 9, 1], [-1, -1, 0, 1])
+    assert Lookup().tree([], 5, 5) == ([], []) and Lookup().tree([4], 5, 5) == ([], [])
+    # a run that reaches the history's end is shorter
+    assert Lookup(1, 1).tree([6, 6], 5, 5) == ([6], [-1])
+
+
+def test_engine_with_drafts_returns_turns_of_the_asked_length():
+    """A stand-in generator whose tokens repeat with period five and whose tree steps confirm what is right."""
+    from paper_2608_22167_amd import rollout
+
+    class Seq:
+        def __init__(self, sid):
+            self.sid, self.history, self.pending = sid, [], []
+
+    class StandIn:
+        def __init__(self):
+            self.seqs, self.held, self.tree_steps = {}, {}, 0
+
+        def add(self, sid, tokens):
+            self.seqs.setdefault(sid, Seq(sid)).pending.extend(tokens)
+
+        def hold(self, sid):
+            self.held[sid] = self.seqs[sid].pending[:]
+            self.seqs[sid].pending.clear()
+
+        def resume(self, sid, obs):
+            self.add(sid, self.held.pop(sid) + list(obs))
+
+        def release(self, sid):
+            self.seqs.pop(sid)
+            self.held.pop(sid, None)
+
+        @staticmethod
+        def token(sid, pos):
+            return 100 * sid + pos % 5
+
+        def _draw(self, s):
+            t = self.token(s.sid, len(s.history))
+            s.pending = [t]
+            return t, -1.0
+
+        def step(self):
+            out = {}
+            for s in self.seqs.values():
+                if s.pending:
+                    s.history += s.pending
+                    out[s.sid] = self._draw(s)
+            return out
+
+        def step_tree(self, drafts):
+            self.tree_steps += 1
+            out = {}
+            for s in self.seqs.values():
+                if len(s.pending) != 1:
+                    continue
+                tokens, parents = drafts[s.sid]
+                assert len(tokens) <= 7
+                s.history += s.pending
+                drawn, at = [self._draw(s)], -1
+                while True:
+                    kids = [i for i, p in enumerate(parents) if p == at and tokens[i] == drawn[-1][0]]
+                    if not kids:
+                        break
+                    at = kids[0]
+                    s.history += s.pending
+                    drawn.append(self._draw(s))
+                out[s.sid] = drawn
+            return out
+
+    gen = StandIn()
+    eng = rollout.Engine(gen, draft_nodes=7)
+    try:
+        for turn, n in enumerate((30, 1, 12)):
+            futures = {sid: eng.generate(sid, [100 * sid + 9] * 3, n) for sid in (1, 2)}
+            for sid, f in futures.items():
+                got = f.result(timeout=30)
+                assert len(got) == n
+        assert gen.tree_steps > 0 and eng.tokens == 2 * (30 + 1 + 12) and eng.steps < eng.tokens / 2
+        for sid in (1, 2):
+            h = gen.seqs[sid].history
+            assert all(h[i] in (100 * sid + 9, gen.token(sid, i)) for i in range(len(h)))
+            eng.release(sid).result(timeout=30)
+        assert not eng.lookups
+    finally:
+        eng.close()
