@@ -472,7 +472,7 @@ int plan_tree(const mcpu_layer_cfg* c, const mcpu_kv_pool* pool, int batch, int 
   if (hcu[0] != 0) return fail(MCPU_EINVAL, "host_cu_q[0] must be 0");
   auto pages_of = [&](int b, int n) {
     const int lo = c->window > 0 ? std::max(0, hsl[b] - c->window + 1) : 0;
-    return n > 0 ? (hsl[b] + n - 1) / PAGE_SIZE - lo / PAGE_SIZE + 1 : 0;
+    return n > 0 ? (int)(((long long)hsl[b] + n - 1) / PAGE_SIZE) - lo / PAGE_SIZE + 1 : 0;
   };
   long long total = 0;
   int longest = 0;

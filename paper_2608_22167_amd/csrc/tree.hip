@@ -337,10 +337,7 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(TreeAttn P, int tiles) {
 #pragma unroll
   for (int n = 0; n < D / 16; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  Page cur, nxt;
-  fetch(cur, it.pg0);
-  for (int pg = it.pg0; pg < it.pg1; ++pg) {
-    fetch(nxt, pg + 1);
+  auto attend = [&](Page& cur, int pg) __attribute__((always_inline)) {
     f32x4 sc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int cc = 0; cc < D / 32; ++cc) sc = mma32(cur.k[cc], qf[cc], sc);
@@ -388,7 +385,20 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(TreeAttn P, int tiles) {
           }
       }
     }
-    cur = nxt;
+  };
+  // four pages in flight, as short contexts are latency alone (three trees over up to 512 cached tokens, fp32: 7.4 us,
+  // 9.9 with one page ahead)
+  constexpr int PF = 4;
+  Page ring[PF];
+#pragma unroll
+  for (int u = 0; u < PF; ++u) fetch(ring[u], it.pg0 + u);
+  for (int pg = it.pg0; pg < it.pg1; pg += PF) {
+#pragma unroll
+    for (int u = 0; u < PF; ++u) {
+      if (pg + u >= it.pg1) break;
+      attend(ring[u], pg + u);
+      fetch(ring[u], pg + u + PF);
+    }
   }
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
@@ -1163,7 +1173,7 @@ __global__ __launch_bounds__(64) void tree_accept_kernel(TreeAccept P) {
   const int b = blockIdx.x, lane = lane_id();
   const int t0 = P.cu_q[b], n = P.cu_q[b + 1] - t0;
   int count = 0, last = -1;
-  if (n < 0 || n > TREE_MAX_NODES || t0 < 0 || t0 + n > P.n_tokens) {
+  if (n < 0 || n > TREE_MAX_NODES || t0 < 0 || t0 > P.n_tokens - n) {
     if (lane == 0) set_error(P.err, 8);
   } else if (n > 0) {
     const bool in = lane < n;

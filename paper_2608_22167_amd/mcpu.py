@@ -152,6 +152,36 @@ def _stream(stream=None):
     return ctypes.c_void_p(s.cuda_stream)
 
 
+# The calls on trees and pages are a few microseconds on the GPU, so their marshalling
+# is kept short: pointers and the raw stream without objects in between.
+
+
+def _buf(t, n, dtype=torch.int32) -> int:
+    """Address of a contiguous device tensor of at least n elements of a type."""
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous() or not t.is_cuda:
+        raise McpuError(MCPU_EINVAL, f"a contiguous {dtype} tensor of {n} elements or more on the GPU is needed, "
+                                     f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+    return t.data_ptr()
+
+
+def _host(a: np.ndarray) -> int:
+    """Address of a contiguous host array."""
+    return ctypes.addressof(ctypes.c_char.from_buffer(a)) if a.size and a.flags.writeable else a.ctypes.data
+
+
+def _stream_on(t, stream=None) -> int:
+    """The stream to launch on: `stream`, or the current one; the tensors have to live on the current device."""
+    dev = t.get_device()
+    if dev != torch.cuda.current_device():
+        raise McpuError(MCPU_EINVAL, f"tensors on device {dev}, current device {torch.cuda.current_device()}")
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _cfg_for(shape, pool):
+    """The call's mcpu_layer_cfg: the pool's own where it was made for this shape."""
+    return ctypes.byref(pool.cfg if shape is pool.shape else make_cfg(shape))
+
+
 def _host_i32(a) -> Optional[np.ndarray]:
     if a is None:
         return None
@@ -309,12 +339,11 @@ def _handles(pools):
 
 def kv_pages_copy(pools, src, dst, host_src, host_dst, workspace, stream=None):
     """Page src[i] -> page dst[i] in every pool of `pools` (layers that share the ids)."""
-    hs, hd = _host_i32(host_src), _host_i32(host_dst)
-    n = int(src.shape[0])
-    if len(hs) != n or len(hd) != n or int(dst.shape[0]) != n:
+    hs, hd, n = _host_i32(host_src), _host_i32(host_dst), src.shape[0]
+    if hs.size != n or hd.size != n or dst.shape[0] != n:
         raise McpuError(MCPU_EINVAL, "src, dst and their host copies differ in length")
-    _check(lib().kv_pages_copy(_handles(pools), len(pools), n, _ptr(src), _ptr(dst), _ptr(hs), _ptr(hd),
-                               _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+    _check(lib().kv_pages_copy(_handles(pools), len(pools), n, _buf(src, n), _buf(dst, n), _host(hs), _host(hd),
+                               workspace.data_ptr(), workspace.nbytes, _stream_on(src, stream)))
 
 
 def workspace(nbytes: int, device="cuda") -> torch.Tensor:
@@ -342,28 +371,39 @@ def tree_attention_workspace_size(shape, max_batch, max_tokens) -> int:
     return lib().tree_attention_workspace_size(ctypes.byref(cfg), max_batch, max_tokens)
 
 
+def _tree_batch(page_table, host_seq_lens, host_cu_q):
+    """Host lengths and row offsets, and the batch and width of the page table they have to fit."""
+    hs, hc = _host_i32(host_seq_lens), _host_i32(host_cu_q)
+    batch, max_pages = page_table.shape
+    if hs.size != batch or hc.size != batch + 1:
+        raise McpuError(MCPU_EINVAL, f"host copies of {hs.size} lengths and {hc.size} row offsets for {batch} sequences")
+    return hs, hc, batch, max_pages
+
+
 def tree_attention(shape, sinks, pool: KVPool, page_table, seq_lens, cu_q, parents, host_seq_lens, host_cu_q,
                    q, o, workspace, stream=None):
-    cfg = make_cfg(shape)
-    hs, hc = _host_i32(host_seq_lens), _host_i32(host_cu_q)
-    _check(lib().tree_attention(ctypes.byref(cfg), _ptr(sinks), pool.handle, int(seq_lens.shape[0]),
-                                _ptr(page_table), int(page_table.shape[1]), _ptr(seq_lens), _ptr(cu_q),
-                                _ptr(parents), _ptr(hs), _ptr(hc), _ptr(q), _ptr(o), _ptr(workspace),
-                                workspace.numel() * workspace.element_size(), _stream(stream)))
+    hs, hc, batch, max_pages = _tree_batch(page_table, host_seq_lens, host_cu_q)
+    n, width, dt = int(hc[batch]), shape.n_q_heads * shape.head_dim, shape.torch_dtype
+    _check(lib().tree_attention(_cfg_for(shape, pool), _ptr(sinks), pool.handle, batch,
+                                _buf(page_table, batch * max_pages), max_pages, _buf(seq_lens, batch),
+                                _buf(cu_q, batch + 1), _buf(parents, n), _host(hs), _host(hc), _buf(q, n * width, dt),
+                                _buf(o, n * width, dt), workspace.data_ptr(), workspace.nbytes,
+                                _stream_on(q, stream)))
 
 
 def tree_accept(cu_q, parents, draft, sampled, path, n_path, next_tokens, workspace, stream=None):
-    _check(lib().tree_accept(int(cu_q.shape[0]) - 1, int(parents.shape[0]), _ptr(cu_q), _ptr(parents), _ptr(draft),
-                             _ptr(sampled), _ptr(path), _ptr(n_path), _ptr(next_tokens), _ptr(workspace),
-                             workspace.numel() * workspace.element_size(), _stream(stream)))
+    batch, n = cu_q.shape[0] - 1, parents.shape[0]
+    _check(lib().tree_accept(batch, n, _buf(cu_q, 1), _buf(parents, n), _buf(draft, n), _buf(sampled, n),
+                             _buf(path, n), _buf(n_path, batch), _buf(next_tokens, batch), workspace.data_ptr(),
+                             workspace.nbytes, _stream_on(parents, stream)))
 
 
 def kv_tree_commit(pools, page_table, seq_lens, cu_q, path, n_path, workspace, stream=None):
     """Keep an accepted path in every pool of `pools` (the layers that page_table belongs to)."""
-    _check(lib().kv_tree_commit(_handles(pools), len(pools), int(seq_lens.shape[0]), _ptr(page_table),
-                                int(page_table.shape[1]), _ptr(seq_lens), _ptr(cu_q), int(path.shape[0]), _ptr(path),
-                                _ptr(n_path), _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                _stream(stream)))
+    (batch, max_pages), n = page_table.shape, path.shape[0]
+    _check(lib().kv_tree_commit(_handles(pools), len(pools), batch, _buf(page_table, batch * max_pages), max_pages,
+                                _buf(seq_lens, batch), _buf(cu_q, batch + 1), n, _buf(path, n), _buf(n_path, batch),
+                                workspace.data_ptr(), workspace.nbytes, _stream_on(path, stream)))
 
 
 def moe_forward_workspace_size(shape, max_tokens) -> int:
@@ -406,14 +446,15 @@ def decode_layer_tree(shape, weights: DeviceWeights, pool: KVPool, page_table, s
                       host_cu_q, x_in, x_out, topk_idx=None, topk_w=None, taps: Optional[Taps] = None,
                       workspace=None, stream=None):
     """decode_layer where each sequence's new tokens are a tree of drafted tokens."""
-    cfg = make_cfg(shape)
-    hs, hc = _host_i32(host_seq_lens), _host_i32(host_cu_q)
-    _check(lib().decode_layer_tree(ctypes.byref(cfg), ctypes.byref(weights.struct), pool.handle,
-                                   int(seq_lens.shape[0]), _ptr(page_table), int(page_table.shape[1]),
-                                   _ptr(seq_lens), _ptr(cu_q), _ptr(parents), _ptr(hs), _ptr(hc), _ptr(x_in),
-                                   _ptr(x_out), _ptr(topk_idx), _ptr(topk_w),
-                                   ctypes.byref(taps) if taps is not None else None,
-                                   _ptr(workspace), workspace.numel(), _stream(stream)))
+    hs, hc, batch, max_pages = _tree_batch(page_table, host_seq_lens, host_cu_q)
+    n = int(hc[batch])
+    _check(lib().decode_layer_tree(_cfg_for(shape, pool), ctypes.byref(weights.struct), pool.handle, batch,
+                                   _buf(page_table, batch * max_pages), max_pages, _buf(seq_lens, batch),
+                                   _buf(cu_q, batch + 1), _buf(parents, n), _host(hs), _host(hc),
+                                   _buf(x_in, n * shape.hidden, torch.float32),
+                                   _buf(x_out, n * shape.hidden, torch.float32),
+                                   _ptr(topk_idx), _ptr(topk_w), ctypes.byref(taps) if taps is not None else None,
+                                   workspace.data_ptr(), workspace.nbytes, _stream_on(x_in, stream)))
 
 
 def decode_layer_noalloc(shape, weights: DeviceWeights, pool: KVPool, page_table, seq_lens, cu_q, host_seq_lens,

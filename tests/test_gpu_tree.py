@@ -234,6 +234,91 @@ def test_attention_on_another_stream_and_used_workspace():
     assert torch.equal(d.run(), d.run(ws=ws))
 
 
+# Many KV heads make a batch large (more than 12288 (page, head) pairs) at a length that the 64-bit definition can
+# follow: 2 x 20 columns take the two-column-pair form without a stage, 2 x 50 and 4 x 40 the staged ones.
+@pytest.mark.parametrize("layout,n", [((64, 32, 64, "bf16"), 20), ((64, 32, 64, "bf16"), 50), ((128, 32, 64, "bf16"), 40),
+                                      ((32, 32, 64, "bf16"), 3)], ids=str)
+@pytest.mark.parametrize("window", [0, 2000])
+def test_attention_of_large_batches(layout, n, window):
+    rng = np.random.default_rng(n)
+    Case(layout, [2500, 2481, 2500 if window else 1300, 0], trees(rng, [n, n - 1, n, 1]), window, 26).check()
+
+
+@pytest.mark.parametrize("layout", [LAYOUTS[0], LAYOUTS[3]], ids=str)
+@pytest.mark.parametrize("longest", [300, 3000])
+def test_attention_of_more_than_256_sequences(layout, longest):
+    """Beyond the batch whose row offsets one workgroup scans: short trees, and some that are split."""
+    rng = np.random.default_rng(longest)
+    seq = rng.integers(0, 60, 301)
+    seq[[7, 200, 300]] = longest
+    Case(layout, seq, trees(rng, rng.integers(0, 5, 301)), 0, 27).check()
+
+
+def test_attention_in_two_graphs_that_share_a_workspace():
+    """Two captured calls of different batches on one workspace, replayed in turn with eager calls between them."""
+    rng = np.random.default_rng(28)
+    cases = [Case(LAYOUTS[2], [2000, 10], trees(rng, [30, 9]), 0, 29), Case(LAYOUTS[2], [300, 5, 900], trees(rng, [7, 64, 3]), 0, 30)]
+    want = [c.run() for c in cases]
+    ws = mcpu.workspace(max(mcpu.tree_attention_workspace_size(c.shape, len(c.seq), c.T) for c in cases))
+    up = lambda a: torch.from_numpy(np.ascontiguousarray(a, np.int32)).cuda()  # noqa: E731
+    graphs, outs, keep = [], [], []
+    for c in cases:
+        s = c.shape
+        page = (c.n_pages, s.n_kv_heads, PAGE, s.head_dim)
+        pool = mcpu.KVPool(s, c.k.cuda().view(page), c.v.cuda().view(page))
+        o = torch.zeros((c.T, s.n_q_heads * s.head_dim), dtype=s.torch_dtype, device="cuda")
+        args = (s, c.sinks.cuda(), pool, up(c.table), up(c.seq), up(c.cu), up(c.par), c.seq, c.cu, c.q.cuda(), o, ws)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            mcpu.tree_attention(*args)
+        graphs.append(g), outs.append(o), keep.append(args)
+    for i in (0, 1, 1, 0, 1, 0):
+        outs[i].zero_()
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[i].cpu().view(want[i].shape), want[i])
+        cases[1 - i].run(ws=ws)
+    assert mcpu.mcpu_check_device_errors(ws) == 0
+
+
+def test_refusals_of_tensors():
+    """Types, lengths, strides and devices that the calls would misread."""
+    c = Case(LAYOUTS[3], [40, 9], trees(np.random.default_rng(31), [6, 4]), 0, 32)
+    s, n = c.shape, c.T
+    page = (c.n_pages, s.n_kv_heads, PAGE, s.head_dim)
+    pool = mcpu.KVPool(s, c.k.cuda().view(page), c.v.cuda().view(page))
+    up = lambda a: torch.from_numpy(np.ascontiguousarray(a, np.int32)).cuda()  # noqa: E731
+    ws = mcpu.workspace(mcpu.tree_attention_workspace_size(s, 2, n))
+    good = dict(table=up(c.table), seq=up(c.seq), cu=up(c.cu), par=up(c.par), hseq=c.seq, hcu=c.cu, q=c.q.cuda(),
+                o=torch.zeros((n, 512), dtype=torch.bfloat16, device="cuda"))
+    call = lambda **kw: (lambda a: mcpu.tree_attention(s, None, pool, *a.values(), ws))({**good, **kw})  # noqa: E731
+    call()
+    wide = torch.zeros((n, 1024), dtype=torch.bfloat16, device="cuda")
+    for bad in (dict(seq=good["seq"].long()), dict(seq=good["seq"][:1]), dict(cu=good["cu"][:2]), dict(par=good["par"][:-1]),
+                dict(par=up(np.repeat(c.par, 2))[::2]), dict(q=good["q"].float()), dict(q=good["q"][:-1]), dict(o=wide[:, :512]),
+                dict(q=good["q"].cpu()), dict(seq=good["seq"].cpu()), dict(hseq=c.seq[:1]), dict(hcu=c.cu[:2]),
+                dict(table=good["table"].t()), dict(o=good["o"].view(torch.float16))):
+        with pytest.raises(mcpu.McpuError):
+            call(**bad)
+    path, two = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    for i, bad in ((1, good["par"].long()), (2, good["par"][:-1]), (4, path[:-1]), (5, two[:1]), (6, two.cpu())):
+        a = [good["cu"], good["par"], path, path, path.clone(), two, two.clone()]
+        a[i] = bad
+        with pytest.raises(mcpu.McpuError):
+            mcpu.tree_accept(*a, ws)
+    for i, bad in ((0, good["table"].cpu()), (1, good["seq"][:1]), (2, good["cu"].long()), (3, path.cpu()), (4, two[:1])):
+        a = [good["table"], good["seq"], good["cu"], path, two]
+        a[i] = bad
+        with pytest.raises(mcpu.McpuError):
+            mcpu.kv_tree_commit([pool], *a, ws)
+    for src, hs in ((two.cpu(), [0, 0]), (two.long(), [0, 0]), (two, [0])):
+        with pytest.raises(mcpu.McpuError):
+            mcpu.kv_pages_copy([pool], src, two, np.array(hs, np.int32), np.array([1, 2], np.int32), ws)
+    torch.cuda.synchronize()
+    assert mcpu.mcpu_check_device_errors(ws) == 0
+
+
 def test_attention_pools_off_16_byte_boundaries():
     """Pools that start 8 bytes past a 16-byte boundary."""
     rng = np.random.default_rng(22)

@@ -114,6 +114,40 @@ def test_layer_over_trees_of_mxfp4_and_of_chains():
     assert torch.equal(a[3], b[3]) and torch.equal(a[4], b[4])  # the same keys and values, bit for bit
 
 
+def test_layer_over_trees_in_a_graph():
+    """A captured step, replayed with other inputs in the same tensors and eager work in between."""
+    shape = replace(W.GPT_OSS_20B, n_q_heads=16, n_kv_heads=2, hidden=256, ffn_dim=256, n_experts=4, top_k=2)
+    rng = np.random.default_rng(51)
+    seq = np.array([900, 3, 60], np.int32)
+    tr = [R.random_tree(rng, 30, 3), R.random_tree(rng, 5, 2), [-1]]
+    n = np.array([len(t) for t in tr])
+    wl = W.custom(shape, seq, n, 1304, sink_std=0.5)
+    weights = mcpu.DeviceWeights(shape, wl.weights)
+    k, v = wl.k_pool.cuda(), wl.v_pool.cuda()
+    pool = mcpu.KVPool(shape, k, v)
+    x = wl.x_in.cuda()
+    out = torch.empty_like(x)
+    dev = [_up(a) for a in (wl.page_table, seq, wl.cu_q, np.concatenate(tr))]
+    ws = mcpu.workspace(mcpu.decode_layer_tree_workspace_size(shape, 3, int(n.sum())))
+    run = lambda: mcpu.decode_layer_tree(shape, weights, pool, *dev, seq, wl.cu_q, x, out, workspace=ws)  # noqa: E731
+    run()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    first = x.clone()
+    for step in range(4):
+        x.copy_(first.roll(step, 0))
+        run()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in (out, k, v)]
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for t, w in zip((out, k, v), want):
+            assert torch.equal(t, w)
+    assert mcpu.mcpu_check_device_errors(ws) == 0
+
+
 def test_layer_over_trees_reports_positions_past_the_rope_table():
     shape = W.TINY
     wl = W.custom(shape, [20], [8], 1303)

@@ -5,6 +5,7 @@ from dataclasses import replace
 
 import numpy as np
 import pytest
+import torch
 
 from paper_2608_22167_amd import mcpu, workload as W
 from tests import tree_reference as R
@@ -269,3 +270,9 @@ def test_engine_with_drafts_returns_turns_of_the_asked_length():
         assert not eng.lookups
     finally:
         eng.close()
+
+
+def test_tensors_off_the_gpu_are_refused():
+    i = lambda *v: torch.tensor(v, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(mcpu.McpuError):
+        mcpu.tree_accept(i(0, 1), i(-1), i(3), i(4), i(0), i(0), i(0), torch.zeros(256, dtype=torch.uint8))
