@@ -27,21 +27,20 @@ __device__ __forceinline__ int first_page(int len, int window) {
 }
 
 // Sequence b's tree, its pages and its splits; none for an empty tree, for b past
-// the batch and for device arrays that do not fit the call, which raise bit 8 if
-// `report`.
+// the batch and for device arrays that do not fit the call (`bad`, reported as bit 8).
 struct TreeSpan {
   int t0, n, len, pages, splits;
+  bool bad;
 };
-__device__ __forceinline__ TreeSpan tree_span(const TreeArgs& P, int b, bool report) {
+__device__ __forceinline__ TreeSpan tree_span(const TreeArgs& P, int b) {
   const int at = min(b, P.batch - 1);  // loads without a branch, so that several spans' are in flight together
   TreeSpan s;
   s.t0 = P.cu_q[at];
   s.n = P.cu_q[at + 1] - s.t0;
   s.len = P.seq_lens[at];
-  const bool bad = s.n < 0 || s.n > TREE_MAX_NODES || s.t0 < 0 || s.t0 > P.n_tokens - s.n || s.len < 0 ||
-                   (s.n > 0 && (s.len > INT32_MAX - TREE_MAX_NODES || (s.len + s.n - 1) / PAGE >= P.max_pages));
-  if (bad && report) set_error(P.err, 8);
-  s.n = bad || b >= P.batch ? 0 : s.n;
+  s.bad = s.n < 0 || s.n > TREE_MAX_NODES || s.t0 < 0 || s.t0 > P.n_tokens - s.n || s.len < 0 ||
+          (s.n > 0 && (s.len > INT32_MAX - TREE_MAX_NODES || (s.len + s.n - 1) / PAGE >= P.max_pages));
+  s.n = s.bad || b >= P.batch ? 0 : s.n;
   s.pages = s.n > 0 ? (s.len + s.n - 1) / PAGE - first_page(s.len, P.window) + 1 : 0;
   s.splits = (s.pages + P.pps - 1) / P.pps;
   return s;
@@ -68,7 +67,8 @@ __global__ __launch_bounds__(1024) void tree_plan_kernel(TreeArgs P, TreeItem* o
   int items = 0, rows = 0;
   for (int base = 0; base < P.batch; base += 1024) {
     const int b = base + threadIdx.x;
-    const TreeSpan s = tree_span(P, b, true);
+    const TreeSpan s = tree_span(P, b);
+    if (s.bad) set_error(P.err, 8);
     const int incl = wave_incl_scan(s.splits), rincl = wave_incl_scan(rows_of(s));
     __syncthreads();  // sums may still be read for the tile before
     if (lane == 63) {
@@ -116,7 +116,8 @@ __device__ __forceinline__ bool find_item(const TreeArgs& P, int i, TreeItem& it
   bool ok = false;
   it = TreeItem{};
   if (P.n_rows == 0) {
-    const TreeSpan s = tree_span(P, i, true);
+    const TreeSpan s = tree_span(P, i);
+    if (s.bad) set_error(P.err, 8);
     if (uniform(s.n) == 0) return false;
     it = split_of(P, s, i, 0, 0);
     ok = it.splits == 1;
@@ -129,8 +130,9 @@ __device__ __forceinline__ bool find_item(const TreeArgs& P, int i, TreeItem& it
     const int lane = lane_id();
     TreeSpan s[TREE_SCAN / 64];
 #pragma unroll
-    for (int c = 0; c < TREE_SCAN / 64; ++c) s[c] = tree_span(P, 64 * c + lane, false);
+    for (int c = 0; c < TREE_SCAN / 64; ++c) s[c] = tree_span(P, 64 * c + lane);
     int items = 0, rows = 0;
+    bool bad = false;
 #pragma unroll
     for (int c = 0; c < TREE_SCAN / 64; ++c) {
       if (64 * c >= P.batch) break;
@@ -148,11 +150,9 @@ __device__ __forceinline__ bool find_item(const TreeArgs& P, int i, TreeItem& it
       }
       items += __builtin_amdgcn_readlane(incl, 63);
       rows += __builtin_amdgcn_readlane(rincl, 63);
+      bad |= s[c].bad;
     }
-    if (i == 0) {
-      if ((items != P.n_items || rows != P.n_rows) && lane == 0) set_error(P.err, 8);
-      for (int b = lane; b < P.batch; b += 64) tree_span(P, b, true);  // report spans that do not fit
-    }
+    if (i == 0 && (bad || items != P.n_items || rows != P.n_rows)) set_error(P.err, 8);
   }
   it.b = uniform(it.b); it.t0 = uniform(it.t0); it.n = uniform(it.n); it.len = uniform(it.len);
   it.pg0 = uniform(it.pg0); it.pg1 = uniform(it.pg1); it.row0 = uniform(it.row0); it.splits = uniform(it.splits);
@@ -169,9 +169,12 @@ struct Nodes {
   uint64_t seen;
   int depth;
 };
-__device__ __forceinline__ Nodes nodes_of(const TreeArgs& P, const TreeItem& it) {
+__device__ __forceinline__ int parent_of(const TreeArgs& P, const TreeItem& it) {
   const int lane = lane_id();
-  int up = lane < it.n ? P.parents[it.t0 + lane] : -1;
+  return lane < it.n ? P.parents[it.t0 + lane] : -1;
+}
+__device__ __forceinline__ Nodes nodes_of(const TreeArgs& P, const TreeItem& it, int up) {  // up = parent_of(P, it)
+  const int lane = lane_id();
   if (up < -1 || up >= lane) {
     if (lane < it.n) set_error(P.err, 64);
     up = -1;
@@ -208,11 +211,12 @@ __device__ __forceinline__ Nodes nodes_of(const TreeArgs& P, const TreeItem& it)
 __global__ __launch_bounds__(256) void tree_positions_kernel(TreeArgs P, int32_t* rope) {
   const int b = blockIdx.x * 4 + uniform(threadIdx.x >> 6), lane = lane_id();
   if (b >= P.batch) return;
-  const TreeSpan s = tree_span(P, b, true);
+  const TreeSpan s = tree_span(P, b);
+  if (s.bad) set_error(P.err, 8);
   TreeItem it{};
   it.t0 = uniform(s.t0);
   it.n = uniform(s.n);
-  const Nodes d = nodes_of(P, it);
+  const Nodes d = nodes_of(P, it, parent_of(P, it));
   if (lane < it.n) rope[it.t0 + lane] = s.len + d.depth;
 }
 
@@ -300,15 +304,11 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(TreeAttn P, int tiles) {
   if (16 * tile >= cols) return;
   const int c = 16 * tile + hl, node = min(c / G, it.n - 1), head = g * G + c % G;
   const bool valid = c < cols;
-  const Sight sight = sight_of(P, it, nodes_of(P, it), node);
-  if (g == 0 && tile == 0) write_rows(P, it);
+  const int parent = parent_of(P, it);
   Frag<T> qf[D / 32];
   const T* qb = reinterpret_cast<const T*>(P.q) + ((int64_t)(it.t0 + node) * P.hq + head) * D + 8 * grp;
 #pragma unroll
-  for (int cc = 0; cc < D / 32; ++cc) {
-    qf[cc].load(qb + 32 * cc);
-    qf[cc].keep_if(valid);
-  }
+  for (int cc = 0; cc < D / 32; ++cc) qf[cc].load(qb + 32 * cc);
   const T* kpool = reinterpret_cast<const T*>(P.k_pool);
   const T* vpool = reinterpret_cast<const T*>(P.v_pool);
   const int32_t* ptab = P.page_table + (int64_t)it.b * P.max_pages;
@@ -332,6 +332,16 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(TreeAttn P, int tiles) {
 #pragma unroll
     for (int n = 0; n < D / 16; ++n) p.v[n].load(p.vp + (64 * n + lane) * 4);
   };
+  // four pages in flight, as short contexts are latency alone (three trees over up to 512 cached tokens, fp32: 7.4 us,
+  // 9.9 with one page ahead); the first before the tree's ancestors are worked out
+  constexpr int PF = 4;
+  Page ring[PF];
+#pragma unroll
+  for (int u = 0; u < PF; ++u) fetch(ring[u], it.pg0 + u);
+  const Sight sight = sight_of(P, it, nodes_of(P, it, parent), node);
+  if (g == 0 && tile == 0) write_rows(P, it);
+#pragma unroll
+  for (int cc = 0; cc < D / 32; ++cc) qf[cc].keep_if(valid);
   float m = -INFINITY, l = 0.f;
   f32x4 acc[D / 16];
 #pragma unroll
@@ -386,12 +396,6 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(TreeAttn P, int tiles) {
       }
     }
   };
-  // four pages in flight, as short contexts are latency alone (three trees over up to 512 cached tokens, fp32: 7.4 us,
-  // 9.9 with one page ahead)
-  constexpr int PF = 4;
-  Page ring[PF];
-#pragma unroll
-  for (int u = 0; u < PF; ++u) fetch(ring[u], it.pg0 + u);
   for (int pg = it.pg0; pg < it.pg1; pg += PF) {
 #pragma unroll
     for (int u = 0; u < PF; ++u) {
@@ -608,30 +612,6 @@ __global__ __launch_bounds__(64 * NC, NT == 1 ? 4 : 2) void tree_attn_wide_kerne
   const int32_t* ptab = P.page_table + (int64_t)it.b * P.max_pages;
   const int n_steps = (it.pg1 - it.pg0 + 1) / 2;
 
-  const Nodes nodes = nodes_of(P, it);
-  if (g == 0 && tile == 0 && wave == 0) write_rows(P, it);
-
-  // this lane's column in each of the wavefront's tiles
-  const int fc = lane & 31, h = lane >> 5;
-  int node[NT], head[NT];
-  bool valid[NT];
-  Sight sight[NT];
-  Frag<bf16> qf[NT][4];
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const int c = c0 + 32 * j + fc;
-    valid[j] = c < cols;
-    node[j] = min(c / G, it.n - 1);
-    head[j] = g * G + c % G;
-    sight[j] = sight_of(P, it, nodes, node[j]);
-    const bf16* qp = reinterpret_cast<const bf16*>(P.q) + ((int64_t)(it.t0 + node[j]) * P.hq + head[j]) * D + 8 * h;
-#pragma unroll
-    for (int cc = 0; cc < 4; ++cc) {
-      qf[j][cc].load(qp + 16 * cc);
-      qf[j][cc].keep_if(valid[j]);
-    }
-  }
-
   // page ids of steps base .. base + 31, lane i: page pg0 + 2 base + i (the split's last page past its end). A
   // block of IDB steps and the requests ahead of it find their ids in one register; the next block's are
   // loaded a block ahead.
@@ -641,6 +621,24 @@ __global__ __launch_bounds__(64 * NC, NT == 1 ? 4 : 2) void tree_attn_wide_kerne
     return ptab[min(it.pg0 + 2 * base + lane, it.pg1 - 1)];
   };
   int ids = ids_of(0), base = 0;
+  const int parent = parent_of(P, it);
+
+  // this lane's column in each of the wavefront's tiles
+  const int fc = lane & 31, h = lane >> 5;
+  int node[NT], head[NT];
+  bool valid[NT];
+  Frag<bf16> qf[NT][4];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int c = c0 + 32 * j + fc;
+    valid[j] = c < cols;
+    node[j] = min(c / G, it.n - 1);
+    head[j] = g * G + c % G;
+    const bf16* qp = reinterpret_cast<const bf16*>(P.q) + ((int64_t)(it.t0 + node[j]) * P.hq + head[j]) * D + 8 * h;
+#pragma unroll
+    for (int cc = 0; cc < 4; ++cc) qf[j][cc].load(qp + 16 * cc);
+  }
+
   const int64_t page_bytes = (int64_t)P.hkv * PB;
   // piece w of a step, 1 KB: half w % 2 of K of page 0, K of page 1, V of page 0, V of page 1 (w / 2). The 16-byte
   // chunks of V are permuted on the way (128-byte block b of a 512-byte dim tile to b ^ (tile & 1)), so that the
@@ -667,6 +665,21 @@ __global__ __launch_bounds__(64 * NC, NT == 1 ? 4 : 2) void tree_attn_wide_kerne
       __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t)(stg + 1024 * w), 16, vo, 0, 0, POLICY);
     }
   };
+
+  // the first pages before the tree's ancestors are worked out: one round of memory less in front of the first step
+#pragma unroll
+  for (int s = 0; s < TRS - 1; ++s) {
+    request(stage_of(s), s);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  const Nodes nodes = nodes_of(P, it, parent);
+  Sight sight[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    sight[j] = sight_of(P, it, nodes, node[j]);
+#pragma unroll
+    for (int cc = 0; cc < 4; ++cc) qf[j][cc].keep_if(valid[j]);
+  }
 
   constexpr float WEIGHT_LIMIT = 0x1p8f;       // of a lane's 16 weights in a step
   bool odd = false;  // values that are not finite were dropped
@@ -808,11 +821,6 @@ __global__ __launch_bounds__(64 * NC, NT == 1 ? 4 : 2) void tree_attn_wide_kerne
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   };
-#pragma unroll
-  for (int s = 0; s < TRS - 1; ++s) {
-    request(stage_of(s), s);
-    __builtin_amdgcn_sched_barrier(0);
-  }
   publish();
   Scores sc[2];
   if (busy) {
@@ -846,6 +854,7 @@ __global__ __launch_bounds__(64 * NC, NT == 1 ? 4 : 2) void tree_attn_wide_kerne
   }
   __builtin_amdgcn_s_waitcnt(0);  // no load into LDS may outlive the workgroup
 
+  if (g == 0 && tile == 0 && wave == 0) write_rows(P, it);
   if (odd) add_nonfinite<NT>(P, it, g, sight, valid, h, acc);
   finish<NT>(P, it, node, head, valid, h, m_run, l, acc);
 }
@@ -902,11 +911,9 @@ __global__ __launch_bounds__(64, NT == 1 ? 3 : 2) void tree_attn_narrow_kernel(T
       for (int i = 0; i < 4; ++i) st.v[p][i] = ld_stream8(vpool + off[p] + vo + 512 * (i >> 1) + 128 * (i & 1));
   };
 
-  const Nodes nodes = nodes_of(P, it);
-  if (g == 0 && tile == 0) write_rows(P, it);
+  const int parent = parent_of(P, it);
   int node[NT], head[NT];
   bool valid[NT];
-  Sight sight[NT];
   Frag<bf16> qf[NT][4];
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
@@ -914,13 +921,20 @@ __global__ __launch_bounds__(64, NT == 1 ? 3 : 2) void tree_attn_narrow_kernel(T
     valid[j] = c < cols;
     node[j] = min(c / G, it.n - 1);
     head[j] = g * G + c % G;
-    sight[j] = sight_of(P, it, nodes, node[j]);
     const bf16* qp = reinterpret_cast<const bf16*>(P.q) + ((int64_t)(it.t0 + node[j]) * P.hq + head[j]) * D + 8 * h;
 #pragma unroll
-    for (int cc = 0; cc < 4; ++cc) {
-      qf[j][cc].load(qp + 16 * cc);
-      qf[j][cc].keep_if(valid[j]);
-    }
+    for (int cc = 0; cc < 4; ++cc) qf[j][cc].load(qp + 16 * cc);
+  }
+  Step a, b;
+  fetch(a, 0, 0);
+  fetch(b, 1, 1);
+  const Nodes nodes = nodes_of(P, it, parent);
+  Sight sight[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    sight[j] = sight_of(P, it, nodes, node[j]);
+#pragma unroll
+    for (int cc = 0; cc < 4; ++cc) qf[j][cc].keep_if(valid[j]);
   }
   constexpr float WEIGHT_LIMIT = 0x1p8f;
   bool odd = false;  // values that are not finite were dropped
@@ -1011,9 +1025,6 @@ __global__ __launch_bounds__(64, NT == 1 ? 3 : 2) void tree_attn_narrow_kernel(T
   // blocks of 30 steps, whose ids and those of the two steps requested ahead sit in one register; a step past
   // the end reads the last page again and is masked
   constexpr int BLK = 30;
-  Step a, b;
-  fetch(a, 0, 0);
-  fetch(b, 1, 1);
   for (int base = 0;;) {
     const int next = ids_of(base + BLK), stop = min(n_steps, base + BLK);
     int step = base;
@@ -1028,6 +1039,7 @@ __global__ __launch_bounds__(64, NT == 1 ? 3 : 2) void tree_attn_narrow_kernel(T
     base = stop;
     ids = next;
   }
+  if (g == 0 && tile == 0) write_rows(P, it);
   if (odd) add_nonfinite<NT>(P, it, g, sight, valid, h, acc);
   finish<NT>(P, it, node, head, valid, h, m_run, l, acc);
 }
@@ -1095,41 +1107,48 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeCombine P) {
   const int row0 = uniform(tok.x), n = uniform(tok.y), splits = uniform(tok.z);
   // a stale record (device arrays that disagree with the plan) stays inside the partial rows
   if (splits <= 1 || row0 < 0 || n <= 0 || n > TREE_MAX_NODES || (int64_t)row0 + (int64_t)(splits - 1) * n >= P.n_rows) return;
+  const float sink = P.sinks ? P.sinks[h] * LOG2E : 0.f;
   float M = -INFINITY, L = 0.f;
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-  constexpr int U = 4;  // rows in flight per lane
-  for (int k0 = sub; k0 < splits; k0 += U * RW) {
-    float2 ml[U];
-    float4 v[U];
+  // U rows in flight per lane
+  auto join = [&](auto U_) __attribute__((always_inline)) {
+    constexpr int U = decltype(U_)::value;
+    for (int k0 = sub; k0 < splits; k0 += U * RW) {
+      float2 ml[U];
+      float4 v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {  // past the end: the last split again, with no weight
-      const int k = k0 + u * RW;
-      const int64_t row = (int64_t)(row0 + min(k, splits - 1) * n) * P.hq + h;
-      ml[u] = *reinterpret_cast<const float2*>(P.part_ml + 2 * row);
-      v[u] = *reinterpret_cast<const float4*>(P.part_acc + row * D + dim);
-      ml[u].x = k < splits ? ml[u].x : -INFINITY;
+      for (int u = 0; u < U; ++u) {  // past the end: the last split again, with no weight
+        const int k = k0 + u * RW;
+        const int64_t row = (int64_t)(row0 + min(k, splits - 1) * n) * P.hq + h;
+        ml[u] = *reinterpret_cast<const float2*>(P.part_ml + 2 * row);
+        v[u] = *reinterpret_cast<const float4*>(P.part_acc + row * D + dim);
+        ml[u].x = k < splits ? ml[u].x : -INFINITY;
+      }
+      float Mn = M;
+#pragma unroll
+      for (int u = 0; u < U; ++u) Mn = fmaxf(Mn, ml[u].x);
+      const float base = Mn == -INFINITY ? 0.f : Mn, r = __builtin_amdgcn_exp2f(M - base);
+      L *= r;
+      a.x *= r; a.y *= r; a.z *= r; a.w *= r;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool in = k0 + u * RW < splits;  // a row that is not finite keeps its weight
+        const float f = in ? __builtin_amdgcn_exp2f(ml[u].x - base) : 0.f;
+        L += in ? ml[u].y * f : 0.f;
+        a.x += in ? v[u].x * f : 0.f; a.y += in ? v[u].y * f : 0.f;
+        a.z += in ? v[u].z * f : 0.f; a.w += in ? v[u].w * f : 0.f;
+      }
+      M = Mn;
     }
-    float Mn = M;
-#pragma unroll
-    for (int u = 0; u < U; ++u) Mn = fmaxf(Mn, ml[u].x);
-    const float base = Mn == -INFINITY ? 0.f : Mn, r = __builtin_amdgcn_exp2f(M - base);
-    L *= r;
-    a.x *= r; a.y *= r; a.z *= r; a.w *= r;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const bool in = k0 + u * RW < splits;  // a row that is not finite keeps its weight
-      const float f = in ? __builtin_amdgcn_exp2f(ml[u].x - base) : 0.f;
-      L += in ? ml[u].y * f : 0.f;
-      a.x += in ? v[u].x * f : 0.f; a.y += in ? v[u].y * f : 0.f;
-      a.z += in ? v[u].z * f : 0.f; a.w += in ? v[u].w * f : 0.f;
-    }
-    M = Mn;
-  }
+  };
+  if (splits <= RW) join(std::integral_constant<int, 1>{});
+  else if (splits <= 2 * RW) join(std::integral_constant<int, 2>{});
+  else join(std::integral_constant<int, 8>{});
   // join the lane groups, then the sink
   float Mt = M;
 #pragma unroll
   for (int o = LR; o < 64; o <<= 1) Mt = fmaxf(Mt, __shfl_xor(Mt, o, 64));
-  if (P.sinks) Mt = fmaxf(Mt, P.sinks[h] * LOG2E);
+  if (P.sinks) Mt = fmaxf(Mt, sink);
   const float f = __builtin_amdgcn_exp2f(M - (Mt == -INFINITY ? 0.f : Mt));
   L *= f;
   a.x *= f; a.y *= f; a.z *= f; a.w *= f;
@@ -1141,7 +1160,7 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeCombine P) {
     a.z += __shfl_xor(a.z, o, 64);
     a.w += __shfl_xor(a.w, o, 64);
   }
-  if (P.sinks) L += __builtin_amdgcn_exp2f(P.sinks[h] * LOG2E - Mt);
+  if (P.sinks) L += __builtin_amdgcn_exp2f(sink - Mt);
   if (sub != 0) return;
   const float inv = L == 0.f ? 0.f : 1.0f / L;
   store4(reinterpret_cast<T*>(P.o) + ((int64_t)t * P.hq + h) * D + dim,
