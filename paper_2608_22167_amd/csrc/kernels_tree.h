@@ -22,6 +22,7 @@ struct TreeArgs {
   const int32_t* cu_q;      // [batch + 1]
   const int32_t* parents;   // [n_tokens]
   int batch, n_tokens, max_pages, window;
+  int max_nodes;            // of a tree, as the host counted them
   int pps;                  // pages per split
   int n_items, n_rows;      // splits and partial rows as the host counted them, checked on the device; without
                             // partial rows item i is tree i (n_items = batch)
@@ -33,18 +34,18 @@ hipError_t launch_tree_plan(const TreeArgs& p, TreeItem* out, hipStream_t s);
 // How a step's columns (node and query head pairs of one KV head) are dealt out:
 // `cols` of them to each workgroup (each wavefront for TREE_ANY), of which `per_cu`
 // are at work on a compute unit at a time.
-enum TreeKind { TREE_ANY, TREE_NARROW1, TREE_NARROW2, TREE_WIDE1, TREE_WIDE2, TREE_WIDE4 };
+enum TreeKind { TREE_ANY, TREE_NARROW1, TREE_NARROW1_STREAM, TREE_NARROW2, TREE_WIDE1, TREE_WIDE2, TREE_WIDE4 };
 struct TreeForm {
   int kind, cols, per_cu;
 };
-TreeForm tree_attn_form(int dtype, int head_dim, const void* k_pool, const void* v_pool, int cols, bool light);
+TreeForm tree_attn_form(int dtype, int head_dim, const void* k_pool, const void* v_pool, int cols, bool few, bool one_each);
 
 struct TreeAttn : TreeArgs {
   const void* q;  // [n_tokens][Hq][D]
   const void* k_pool;
   const void* v_pool;
   const int32_t* page_table;
-  int n_pages, max_nodes, hq, hkv;
+  int n_pages, hq, hkv;
   TreeForm form;
   float scale_log2;    // log2(e) / sqrt(D)
   const float* sinks;  // [Hq] or nullptr

@@ -492,7 +492,7 @@ int plan_tree(const mcpu_layer_cfg* c, const mcpu_kv_pool* pool, int batch, int 
   const int cols = out->max_nodes * (c->n_q_heads / c->n_kv_heads);
   const bool one_each = longest <= 2 * TREE_PPS_MIN;
   out->form = tree_attn_form(c->dtype, c->head_dim, pool->k, pool->v, cols,
-                             one_each || total * c->n_kv_heads <= 4 * N_CU * TREE_PPS_MIN);
+                             total * c->n_kv_heads <= 4 * N_CU * TREE_PPS_MIN, one_each);
   if (one_each) {  // short trees: no tree is split
     out->pps = 2 * TREE_PPS_MIN;
     out->n_items = batch;
@@ -557,7 +557,7 @@ TreeArgs tree_args(const mcpu_layer_cfg* c, int batch, int max_pages, const int3
                    const int32_t* parents, const TreePlanHost& ph, int32_t* err) {
   TreeArgs a{};
   a.seq_lens = seq_lens; a.cu_q = cu_q; a.parents = parents; a.batch = batch; a.n_tokens = ph.n_tokens;
-  a.max_pages = max_pages; a.window = c->window; a.pps = ph.pps; a.n_items = ph.n_items; a.n_rows = ph.n_rows;
+  a.max_pages = max_pages; a.window = c->window; a.max_nodes = ph.max_nodes; a.pps = ph.pps; a.n_items = ph.n_items; a.n_rows = ph.n_rows;
   a.err = err;
   return a;
 }
@@ -575,7 +575,7 @@ int run_tree_attention(const mcpu_layer_cfg* c, const float* sinks, mcpu_kv_pool
   }
   ta.q = q; ta.k_pool = pool->k; ta.v_pool = pool->v; ta.page_table = page_table; ta.n_pages = pool->n_pages;
   ta.form = ph.form;
-  ta.max_nodes = ph.max_nodes; ta.hq = c->n_q_heads; ta.hkv = c->n_kv_heads;
+  ta.hq = c->n_q_heads; ta.hkv = c->n_kv_heads;
   ta.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c->head_dim));
   ta.sinks = sinks; ta.part_ml = tb.part_ml; ta.part_acc = tb.part_acc; ta.tok = tb.tok; ta.o = o;
   {

@@ -38,7 +38,7 @@ __device__ __forceinline__ TreeSpan tree_span(const TreeArgs& P, int b) {
   s.t0 = P.cu_q[at];
   s.n = P.cu_q[at + 1] - s.t0;
   s.len = P.seq_lens[at];
-  s.bad = s.n < 0 || s.n > TREE_MAX_NODES || s.t0 < 0 || s.t0 > P.n_tokens - s.n || s.len < 0 ||
+  s.bad = s.n < 0 || s.n > P.max_nodes || s.t0 < 0 || s.t0 > P.n_tokens - s.n || s.len < 0 ||
           (s.n > 0 && (s.len > INT32_MAX - TREE_MAX_NODES || (s.len + s.n - 1) / PAGE >= P.max_pages));
   s.n = s.bad || b >= P.batch ? 0 : s.n;
   s.pages = s.n > 0 ? (s.len + s.n - 1) / PAGE - first_page(s.len, P.window) + 1 : 0;
@@ -511,13 +511,122 @@ __device__ __forceinline__ bool drop_nonfinite(u32x4_t (&vf)[2][2]) {
       }
   return true;
 }
+// One lane's column in each of a wavefront's NT tiles: its node and head, what it
+// sees, its query, and the running softmax.
+constexpr float WEIGHT_LIMIT = 0x1p8f;  // of a lane's 16 weights in a step
+template <int NT>
+struct Columns {
+  int node[NT], head[NT];
+  bool valid[NT];
+  Sight sight[NT];
+  Frag<bf16> qf[NT][4];
+  float m_run[NT], m_sub[NT], limit[NT], l[NT];  // limit: -inf until a key is visible
+  f32x16 acc[2][NT];                             // [dim tile][column tile]
+  bool odd;                                      // values that are not finite were dropped
+
+  // the columns from c0 on, and the loads of their queries
+  __device__ __forceinline__ void request(const TreeAttn& P, const TreeItem& it, int g, int c0) {
+    const int G = P.hq / P.hkv, lane = lane_id(), fc = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int c = c0 + 32 * j + fc;
+      valid[j] = c < it.n * G;
+      node[j] = min(c / G, it.n - 1);
+      head[j] = g * G + c % G;
+      const bf16* qp = reinterpret_cast<const bf16*>(P.q) + ((int64_t)(it.t0 + node[j]) * P.hq + head[j]) * 64 + 8 * h;
+#pragma unroll
+      for (int cc = 0; cc < 4; ++cc) qf[j][cc].load(qp + 16 * cc);
+    }
+  }
+  __device__ __forceinline__ void start(const TreeAttn& P, const TreeItem& it, int parent) {
+    const Nodes nodes = nodes_of(P, it, parent);
+    odd = false;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      sight[j] = sight_of(P, it, nodes, node[j]);
+#pragma unroll
+      for (int cc = 0; cc < 4; ++cc) qf[j][cc].keep_if(valid[j]);
+      m_run[j] = -INFINITY;
+      m_sub[j] = 0.f;
+      limit[j] = -INFINITY;
+      l[j] = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < 2; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[dt][j][e] = 0.f;
+    }
+  }
+  // S^T of 32 keys
+  __device__ __forceinline__ void scores(f32x16 (&t)[NT], const u32x4_t (&kf)[4]) const {
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) t[j][e] = 0.f;
+#pragma unroll
+    for (int cc = 0; cc < 4; ++cc)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        t[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[cc]),
+                                                       __builtin_bit_cast(bf16x8_t, qf[j][cc].v), t[j], 0, 0, 0);
+  }
+  // hide what a column does not see of the 32 keys from k0 on; `pages`: the keys whose page is there
+  __device__ __forceinline__ void mask(f32x16 (&t)[NT], int k0, int len, uint32_t pages) const {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const uint32_t vis = valid[j] ? sight[j].keys(k0, len) & pages : ~0u;
+      hide(t[j], vis >> (4 * (lane_id() >> 5)));
+    }
+  }
+  __device__ __forceinline__ void weights(const f32x16 (&t)[NT], float scale_log2, u32x4_t (&pw)[NT][2], float (&sum)[NT]) const {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) sum[j] = weigh(t[j], scale_log2, m_sub[j], pw[j]);
+  }
+  // The maximum only has to keep the weights in range, so it is raised when a step's sum says that they are not, and
+  // until a column has seen a key; the weights are then formed again.
+  __device__ __forceinline__ void raise(const f32x16 (&t)[NT], float scale_log2, u32x4_t (&pw)[NT][2], float (&sum)[NT]) {
+    bool any = false;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) any |= sum[j] > limit[j];
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(any) != 0, 0)) {  // wave-uniform; the empty asm keeps it a branch
+      asm volatile("");
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        // a column's own lanes decide, so that its bits do not depend on the columns beside it
+        const uint32_t o = sum[j] > limit[j];
+        auto so = __builtin_amdgcn_permlane32_swap(o, o, false, false);
+        const float m_new = (so[0] | so[1]) ? fmaxf(m_run[j], largest(t[j]) * scale_log2) : m_run[j];
+        const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[j] - m_new);
+        l[j] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt) acc[dt][j] *= alpha;
+        m_run[j] = m_new;
+        m_sub[j] = m_new == -INFINITY ? 0.f : m_new;  // masked scores give 2^-inf = 0
+        limit[j] = m_new == -INFINITY ? -INFINITY : WEIGHT_LIMIT;
+      }
+      weights(t, scale_log2, pw, sum);
+    }
+  }
+  // O^T += V^T P^T
+  __device__ __forceinline__ void add(const u32x4_t (&vf)[2][2], const u32x4_t (&pw)[NT][2], const float (&sum)[NT]) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      l[j] += sum[j];
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt)
+          acc[dt][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf[p][dt]),
+                                                               __builtin_bit_cast(bf16x8_t, pw[j][p]), acc[dt][j], 0, 0, 0);
+    }
+  }
+};
 // The steps with masked keys once more, for values that are not finite: added to the
 // accumulators of the columns that see them, which makes those infinite or NaN as
 // any positive weight does. Steps without masked keys need no such care.
 template <int NT>
-__device__ __forceinline__ void add_nonfinite(const TreeAttn& P, const TreeItem& it, int g, const Sight (&sight)[NT],
-                                              const bool (&valid)[NT], int h, f32x16 (&acc)[2][NT]) {
+__device__ __forceinline__ void add_nonfinite(const TreeAttn& P, const TreeItem& it, int g, Columns<NT>& c) {
   constexpr int D = 64;
+  const int h = lane_id() >> 5;
   const int32_t* ptab = P.page_table + (int64_t)it.b * P.max_pages;
   for (int pg = it.pg0; pg < it.pg1; ++pg) {
     const int k0 = pg * PAGE, id = uniform(ptab[pg]);
@@ -537,56 +646,140 @@ __device__ __forceinline__ void add_nonfinite(const TreeAttn& P, const TreeItem&
           const bool bad = (bits & 0x7F80u) == 0x7F80u;
 #pragma unroll
           for (int j = 0; j < NT; ++j)
-            acc[dt][j][e] += bad & valid[j] & sight[j].key(k0 + slot, it.len, it.n) ? bf16_to_f32(bits) : 0.f;
+            c.acc[dt][j][e] += bad & c.valid[j] & c.sight[j].key(k0 + slot, it.len, it.n) ? bf16_to_f32(bits) : 0.f;
         }
   }
 }
 // the lane's dims of each column: a partial row, or o with the sink
 template <int NT>
-__device__ __forceinline__ void finish(const TreeAttn& P, const TreeItem& it, const int (&node)[NT], const int (&head)[NT],
-                                       const bool (&valid)[NT], int h, const float (&m_run)[NT], const float (&l)[NT],
-                                       const f32x16 (&acc)[2][NT]) {
+__device__ __forceinline__ void finish(const TreeAttn& P, const TreeItem& it, const Columns<NT>& c) {
   constexpr int D = 64;
+  const int h = lane_id() >> 5;
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
-    const uint32_t u = __float_as_uint(l[j]);
+    const uint32_t u = __float_as_uint(c.l[j]);
     auto sw = __builtin_amdgcn_permlane32_swap(u, u, false, false);
     float l_tot = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-    if (!valid[j]) continue;
+    if (!c.valid[j]) continue;
     if (it.splits > 1) {
-      const int64_t row = (int64_t)(it.row0 + node[j]) * P.hq + head[j];
-      if (h == 0) *reinterpret_cast<float2*>(P.part_ml + 2 * row) = make_float2(m_run[j], l_tot);
+      const int64_t row = (int64_t)(it.row0 + c.node[j]) * P.hq + c.head[j];
+      if (h == 0) *reinterpret_cast<float2*>(P.part_ml + 2 * row) = make_float2(c.m_run[j], l_tot);
 #pragma unroll
       for (int dt = 0; dt < 2; ++dt)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
           *reinterpret_cast<float4*>(P.part_acc + row * D + 32 * dt + 8 * q + 4 * h) =
-              make_float4(acc[dt][j][4 * q], acc[dt][j][4 * q + 1], acc[dt][j][4 * q + 2], acc[dt][j][4 * q + 3]);
+              make_float4(c.acc[dt][j][4 * q], c.acc[dt][j][4 * q + 1], c.acc[dt][j][4 * q + 2], c.acc[dt][j][4 * q + 3]);
       continue;
     }
     float f = 1.0f;
     if (P.sinks) {
-      const float sk = P.sinks[head[j]] * LOG2E, M = fmaxf(m_run[j], sk);
-      f = m_run[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[j] - M);
+      const float sk = P.sinks[c.head[j]] * LOG2E, M = fmaxf(c.m_run[j], sk);
+      f = c.m_run[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(c.m_run[j] - M);
       l_tot = l_tot * f + __builtin_amdgcn_exp2f(sk - M);
     }
     const float inv = l_tot == 0.f ? 0.f : f / l_tot;
-    bf16* o = reinterpret_cast<bf16*>(P.o) + ((int64_t)(it.t0 + node[j]) * P.hq + head[j]) * D + 4 * h;
+    bf16* o = reinterpret_cast<bf16*>(P.o) + ((int64_t)(it.t0 + c.node[j]) * P.hq + c.head[j]) * D + 4 * h;
 #pragma unroll
     for (int dt = 0; dt < 2; ++dt)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        store4(o + 32 * dt + 8 * q, make_float4(acc[dt][j][4 * q] * inv, acc[dt][j][4 * q + 1] * inv,
-                                                acc[dt][j][4 * q + 2] * inv, acc[dt][j][4 * q + 3] * inv));
+        store4(o + 32 * dt + 8 * q, make_float4(c.acc[dt][j][4 * q] * inv, c.acc[dt][j][4 * q + 1] * inv,
+                                                c.acc[dt][j][4 * q + 2] * inv, c.acc[dt][j][4 * q + 3] * inv));
   }
+}
+
+// A stage holds K of a step's two pages, then V of both, as in the pool but for the
+// 16-byte chunks of V: 128-byte block b of a 512-byte dim tile sits at b ^ (tile & 1),
+// so that the lanes of a half tile read all banks.
+constexpr uint32_t STAGE_PAGE = 2 * PAGE * 64;  // bytes of K (or V) of a page of one KV head
+// a step's key fragments: key l % 32 (page l / 16 % 2), dims 8 h .. of a 16-dim chunk
+__device__ __forceinline__ void stage_keys(u32x4_t (&kf)[4], const uint8_t* stg) {
+  const int fc = lane_id() & 31, h = lane_id() >> 5;
+  const uint32_t ko = (fc >> 4) * STAGE_PAGE + ((h * 16 + (fc & 15)) * 16);
+#pragma unroll
+  for (int cc = 0; cc < 4; ++cc) kf[cc] = *reinterpret_cast<const u32x4_t*>(stg + ko + 512 * cc);
+}
+// The softmax and the value products of the step at page pg from its scores `sc` and
+// its stage, and the scores `sn` of the next step from the stage behind it; ok: its
+// pages are there.
+template <int NT>
+__device__ __forceinline__ void attend_stage(const TreeAttn& P, const TreeItem& it, Columns<NT>& col, f32x16 (&sc)[NT],
+                                             f32x16 (&sn)[NT], const uint8_t* stg, const uint8_t* nxt, int pg,
+                                             const bool (&ok)[2]) {
+  const int lane = lane_id(), fc = lane & 31, h = lane >> 5;
+  u32x4_t kf[4];
+  stage_keys(kf, nxt);
+  const int k0 = pg * PAGE;
+  const bool second = pg + 1 < it.pg1;
+  const bool edge = k0 + 2 * PAGE > it.len || (P.window > 0 && k0 < it.len + it.n - P.window) || !ok[0] || !ok[1] || !second;
+  if (__builtin_expect(edge, 0)) {  // wave-uniform; the empty asm keeps it a branch
+    asm volatile("");
+    if ((!ok[0] || (!ok[1] && second)) && lane == 0) set_error(P.err, 1);
+    col.mask(sc, k0, it.len, (ok[0] ? 0xFFFFu : 0u) | (ok[1] && second ? 0xFFFF0000u : 0u));
+  }
+  u32x4_t pw[NT][2];  // [column tile][page]: the weights, packed
+  float sum[NT];
+  __builtin_amdgcn_sched_barrier(0);
+  col.scores(sn, kf);
+  col.weights(sc, P.scale_log2, pw, sum);
+  // the next scores' products among the vector instructions of the weights, 12 each
+#define TREE_MIX                                      \
+  __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  \
+  __builtin_amdgcn_sched_group_barrier(0x402, 12, 0);
+  TREE_MIX TREE_MIX TREE_MIX TREE_MIX
+  if constexpr (NT == 2) { TREE_MIX TREE_MIX TREE_MIX TREE_MIX }
+#undef TREE_MIX
+  col.raise(sc, P.scale_log2, pw, sum);
+  // dim l % 32 of a tile of 32, value rows 4 h .. and 8 + 4 h ..
+  const uint32_t vbase = (fc >> 4) * 512 + (fc & 15) * 8 + (((uint32_t)h ^ ((fc >> 4) & 1)) << 7);
+  u32x4_t vf[2][2];  // [page][dim tile]
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+#pragma unroll
+    for (int dt = 0; dt < 2; ++dt) {
+      const uint8_t* v = stg + (2 + p) * STAGE_PAGE + 1024 * dt + vbase;
+      const u32x2_t a = *reinterpret_cast<const u32x2_t*>(v), c = *reinterpret_cast<const u32x2_t*>(v + 256);
+      vf[p][dt] = __builtin_shufflevector(a, c, 0, 1, 2, 3);
+    }
+  if (__builtin_expect(edge, 0)) {
+    asm volatile("");
+    col.odd |= drop_nonfinite(vf);
+  }
+  col.add(vf, pw, sum);
+}
+// Piece w of a step, 1 KB, into its stage: half w % 2 of K of page 0, K of page 1, V
+// of page 0, V of page 1 (w / 2) of pool page `id`; a `range` of 0 touches no memory.
+template <int POLICY>
+__device__ __forceinline__ void load_piece(const TreeAttn& P, uint8_t* stg, int w, int g, int id, int range) {
+  const int lane = lane_id();
+  const uint8_t* pool = reinterpret_cast<const uint8_t*>(w < 4 ? P.k_pool : P.v_pool) + (int64_t)g * STAGE_PAGE;
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint8_t*>(pool) + id * ((int64_t)P.hkv * STAGE_PAGE), 0, range, 0x00020000);
+  const uint32_t at = 1024u * (w & 1) + 16u * lane;
+  const uint32_t vo = w < 4 ? at : at ^ (((at >> 9) & 1u) << 7);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t)(stg + 1024 * w), 16, vo, 0, 0, POLICY);
+}
+// Hands the stages over: this wavefront's reads of LDS have returned (lgkmcnt), all
+// its loads but the last N have landed, and the empty asm keeps LDS accesses on their
+// side of the barrier.
+template <int N>
+__device__ __forceinline__ void publish_stages() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (N >> 4 << 14));  // vmcnt(N) expcnt(7) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 template <int NC, int NT, int TRS>
 __global__ __launch_bounds__(64 * NC, NT == 1 ? 4 : 2) void tree_attn_wide_kernel(TreeAttn P, int tiles) {
-  constexpr int D = 64, PE = PAGE * D, PB = 2 * PE;  // elements and bytes of a page of one KV head
+  constexpr uint32_t PB = STAGE_PAGE;
   constexpr int LD = 8 / NC;                         // 1 KB loads per wavefront and step
-  // up to 128 columns no other workgroup reads the pages: the streaming policy (5% at 48 trees of 8-16 nodes)
-  constexpr int POLICY = NC * NT <= 4 ? 2 : 0;
+  // where one workgroup takes all columns of a step whose pages no cache holds: the streaming policy (3% at 48
+  // trees of 8-16 nodes)
+  constexpr int POLICY = NC == 2 ? 2 : 0;
   static_assert(TRS % 2 == 0 && TRS <= 6 && 8 % NC == 0, "stages alternate between two score sets");
   __shared__ __align__(1024) uint8_t s0[4 * PB];
   __shared__ __align__(1024) uint8_t s1[4 * PB];
@@ -623,33 +816,16 @@ __global__ __launch_bounds__(64 * NC, NT == 1 ? 4 : 2) void tree_attn_wide_kerne
   int ids = ids_of(0), base = 0;
   const int parent = parent_of(P, it);
 
-  // this lane's column in each of the wavefront's tiles
-  const int fc = lane & 31, h = lane >> 5;
-  int node[NT], head[NT];
-  bool valid[NT];
-  Frag<bf16> qf[NT][4];
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const int c = c0 + 32 * j + fc;
-    valid[j] = c < cols;
-    node[j] = min(c / G, it.n - 1);
-    head[j] = g * G + c % G;
-    const bf16* qp = reinterpret_cast<const bf16*>(P.q) + ((int64_t)(it.t0 + node[j]) * P.hq + head[j]) * D + 8 * h;
-#pragma unroll
-    for (int cc = 0; cc < 4; ++cc) qf[j][cc].load(qp + 16 * cc);
-  }
+  Columns<NT> col;
+  col.request(P, it, g, c0);
 
-  const int64_t page_bytes = (int64_t)P.hkv * PB;
-  // piece w of a step, 1 KB: half w % 2 of K of page 0, K of page 1, V of page 0, V of page 1 (w / 2). The 16-byte
-  // chunks of V are permuted on the way (128-byte block b of a 512-byte dim tile to b ^ (tile & 1)), so that the
-  // lanes of a half tile read all banks.
   auto page_of = [&](int step, int which, bool& good) __attribute__((always_inline)) {
     const int id = __builtin_amdgcn_readlane(ids, 2 * (step - base) + which);
     good = id >= 0 && id < P.n_pages;
     return good ? id : 0;
   };
-  // request a step's pages; past the split's end the loads have no range and touch no memory, so that every
-  // step counts the same number of them
+  // request a step's pages; past the split's end the loads have no range, so that every step counts the same number
+  // of them
   auto request = [&](uint8_t* stg, int step) __attribute__((always_inline)) {
     const int range = step < n_steps ? PB : 0;
 #pragma unroll
@@ -657,12 +833,7 @@ __global__ __launch_bounds__(64 * NC, NT == 1 ? 4 : 2) void tree_attn_wide_kerne
       const int w = wave * LD + u;
       bool good;
       const int id = page_of(step, (w >> 1) & 1, good);
-      const uint8_t* pool = reinterpret_cast<const uint8_t*>(w < 4 ? P.k_pool : P.v_pool) + (int64_t)g * PB;
-      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
-          const_cast<uint8_t*>(pool) + id * page_bytes, 0, range, 0x00020000);
-      const uint32_t at = 1024u * (w & 1) + 16u * lane;
-      const uint32_t vo = w < 4 ? at : at ^ (((at >> 9) & 1u) << 7);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t)(stg + 1024 * w), 16, vo, 0, 0, POLICY);
+      load_piece<POLICY>(P, stg, w, g, id, range);
     }
   };
 
@@ -672,167 +843,29 @@ __global__ __launch_bounds__(64 * NC, NT == 1 ? 4 : 2) void tree_attn_wide_kerne
     request(stage_of(s), s);
     __builtin_amdgcn_sched_barrier(0);
   }
-  const Nodes nodes = nodes_of(P, it, parent);
-  Sight sight[NT];
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    sight[j] = sight_of(P, it, nodes, node[j]);
-#pragma unroll
-    for (int cc = 0; cc < 4; ++cc) qf[j][cc].keep_if(valid[j]);
-  }
-
-  constexpr float WEIGHT_LIMIT = 0x1p8f;       // of a lane's 16 weights in a step
-  bool odd = false;  // values that are not finite were dropped
-  float m_run[NT], m_sub[NT], limit[NT], l[NT];    // limit: -inf until a key is visible
-  f32x16 acc[2][NT];                           // [dim tile][column tile]
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    m_run[j] = -INFINITY;
-    m_sub[j] = 0.f;
-    limit[j] = -INFINITY;
-    l[j] = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < 2; ++dt)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[dt][j][e] = 0.f;
-  }
-  // fragment addresses: key fc of the step (page fc / 16), dims 8 h .. of a 16-dim chunk; dim fc of a tile of 32,
-  // value rows 4 h .. and 8 + 4 h ..
-  const uint32_t ko = (fc >> 4) * PB + ((h * 16 + (fc & 15)) * 16);
-  const uint32_t vbase = (fc >> 4) * 512 + (fc & 15) * 8 + (((uint32_t)h ^ ((fc >> 4) & 1)) << 7);
-
-  struct Scores {
-    f32x16 t[NT];
-  };
-  auto load_keys = [&](u32x4_t (&kf)[4], const uint8_t* stg) __attribute__((always_inline)) {
-#pragma unroll
-    for (int cc = 0; cc < 4; ++cc) kf[cc] = *reinterpret_cast<const u32x4_t*>(stg + ko + 512 * cc);
-  };
-  auto scores = [&](Scores& sc, const u32x4_t (&kf)[4]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sc.t[j][e] = 0.f;
-#pragma unroll
-    for (int cc = 0; cc < 4; ++cc)
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-        sc.t[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[cc]),
-                                                          __builtin_bit_cast(bf16x8_t, qf[j][cc].v), sc.t[j], 0, 0, 0);
-  };
-  auto start_at = [&](int j, float m) __attribute__((always_inline)) {
-    m_run[j] = m;
-    m_sub[j] = m == -INFINITY ? 0.f : m;  // masked scores give 2^-inf = 0
-    limit[j] = m == -INFINITY ? -INFINITY : WEIGHT_LIMIT;
-  };
-  // a step's softmax and value products from its scores, and the scores of the next step
-  auto attend = [&](Scores& sc, Scores& sn, const uint8_t* stg, const uint8_t* nxt, int step) __attribute__((always_inline)) {
-    u32x4_t kf[4];
-    load_keys(kf, nxt);
-    bool ok[2];
-    page_of(step, 0, ok[0]);
-    page_of(step, 1, ok[1]);
-    const int pg = it.pg0 + 2 * step, k0 = pg * PAGE;
-    const bool second = pg + 1 < it.pg1;
-    const bool edge = k0 + 2 * PAGE > it.len || (P.window > 0 && k0 < it.len + it.n - P.window) || !ok[0] || !ok[1] || !second;
-    uint32_t vis[NT];
-    if (__builtin_expect(edge, 0)) {  // wave-uniform; the empty asm keeps it a branch
-      asm volatile("");
-      if ((!ok[0] || (!ok[1] && second)) && lane == 0) set_error(P.err, 1);
-      const uint32_t pages = (ok[0] ? 0xFFFFu : 0u) | (ok[1] && second ? 0xFFFF0000u : 0u);
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        vis[j] = valid[j] ? sight[j].keys(k0, it.len) & pages : ~0u;
-        hide(sc.t[j], vis[j] >> (4 * h));
-      }
-    }
-    u32x4_t pw[NT][2];  // [column tile][page]: the weights, packed
-    float sum[NT];
-    auto weights = [&]() __attribute__((always_inline)) {
-#pragma unroll
-      for (int j = 0; j < NT; ++j) sum[j] = weigh(sc.t[j], P.scale_log2, m_sub[j], pw[j]);
-    };
-    __builtin_amdgcn_sched_barrier(0);
-    scores(sn, kf);
-    weights();
-    // the next scores' products among the vector instructions of the weights, 12 each
-#define TREE_MIX                                      \
-  __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  \
-  __builtin_amdgcn_sched_group_barrier(0x402, 12, 0);
-    TREE_MIX TREE_MIX TREE_MIX TREE_MIX
-    if constexpr (NT == 2) { TREE_MIX TREE_MIX TREE_MIX TREE_MIX }
-#undef TREE_MIX
-    // The maximum only has to keep the weights in range, so it is raised when a step's sum says that they are
-    // not, and until a column has seen a key; the weights are then formed again.
-    bool raise = false;
-#pragma unroll
-    for (int j = 0; j < NT; ++j) raise |= sum[j] > limit[j];
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(raise) != 0, 0)) {  // wave-uniform (kept a branch)
-      asm volatile("");
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        // a column's own lanes decide, so that its bits do not depend on the columns beside it
-        const uint32_t o = sum[j] > limit[j];
-        auto so = __builtin_amdgcn_permlane32_swap(o, o, false, false);
-        const float m_new = (so[0] | so[1]) ? fmaxf(m_run[j], largest(sc.t[j]) * P.scale_log2) : m_run[j];
-        const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[j] - m_new);
-        l[j] *= alpha;
-#pragma unroll
-        for (int dt = 0; dt < 2; ++dt) acc[dt][j] *= alpha;
-        start_at(j, m_new);
-      }
-      weights();
-    }
-    u32x4_t vf[2][2];  // [page][dim tile]
-#pragma unroll
-    for (int p = 0; p < 2; ++p)
-#pragma unroll
-      for (int dt = 0; dt < 2; ++dt) {
-        const uint8_t* v = stg + (2 + p) * PB + 1024 * dt + vbase;
-        const u32x2_t a = *reinterpret_cast<const u32x2_t*>(v), c = *reinterpret_cast<const u32x2_t*>(v + 256);
-        vf[p][dt] = __builtin_shufflevector(a, c, 0, 1, 2, 3);
-      }
-    if (__builtin_expect(edge, 0)) {
-      asm volatile("");
-      odd |= drop_nonfinite(vf);
-    }
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      l[j] += sum[j];
-#pragma unroll
-      for (int p = 0; p < 2; ++p)
-#pragma unroll
-        for (int dt = 0; dt < 2; ++dt)
-          acc[dt][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf[p][dt]),
-                                                               __builtin_bit_cast(bf16x8_t, pw[j][p]), acc[dt][j], 0, 0, 0);
-    }
-  };
+  col.start(P, it, parent);
 
   // Step s sits in stage s % TRS. In step s its scores are there already; step s + TRS - 1 is requested into the
   // stage step s - 1 left, the scores of step s + 1 are formed, and before the barrier a wavefront waits for its
-  // loads of step s + 2. The barrier hands the stages over: this wavefront's reads of the step's stage have
-  // returned (lgkmcnt), its loads of step s + 2 have landed, and the empty asm keeps LDS accesses on their side.
-  auto publish = [&]() __attribute__((always_inline)) {
-    constexpr int N = LD * (TRS - 3);  // loads that may stay in flight
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (N >> 4 << 14));  // vmcnt(N) expcnt(7) lgkmcnt(0)
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-  };
+  // loads of step s + 2.
+  auto publish = [&]() __attribute__((always_inline)) { publish_stages<LD * (TRS - 3)>(); };
   publish();
-  Scores sc[2];
+  f32x16 sc[2][NT];
   if (busy) {
     u32x4_t kf[4];
-    load_keys(kf, s0);
-    scores(sc[0], kf);
+    stage_keys(kf, s0);
+    col.scores(sc[0], kf);
   }
   auto one = [&](auto U_, int step) __attribute__((always_inline)) {
     constexpr int U = decltype(U_)::value;
     if (step < n_steps) {  // uniform
       request(stage_of((U + TRS - 1) % TRS), step + TRS - 1);
-      if (busy) attend(sc[U % 2], sc[(U + 1) % 2], stage_of(U), stage_of((U + 1) % TRS), step);
+      if (busy) {
+        bool ok[2];
+        page_of(step, 0, ok[0]);
+        page_of(step, 1, ok[1]);
+        attend_stage<NT>(P, it, col, sc[U % 2], sc[(U + 1) % 2], stage_of(U), stage_of((U + 1) % TRS), it.pg0 + 2 * step, ok);
+      }
     }
     publish();
   };
@@ -855,15 +888,15 @@ __global__ __launch_bounds__(64 * NC, NT == 1 ? 4 : 2) void tree_attn_wide_kerne
   __builtin_amdgcn_s_waitcnt(0);  // no load into LDS may outlive the workgroup
 
   if (g == 0 && tile == 0 && wave == 0) write_rows(P, it);
-  if (odd) add_nonfinite<NT>(P, it, g, sight, valid, h, acc);
-  finish<NT>(P, it, node, head, valid, h, m_run, l, acc);
+  if (col.odd) add_nonfinite<NT>(P, it, g, col);
+  finish<NT>(P, it, col);
 }
 
 // The same products for few columns: one wavefront per split, KV head and NT x 32
 // columns, its pages straight to registers, two steps in flight. Nothing is shared,
 // so there is no LDS and no barrier, and the wavefronts of a SIMD hide each other's
 // loads and products.
-template <int NT>
+template <int NT, bool STREAM>
 __global__ __launch_bounds__(64, NT == 1 ? 3 : 2) void tree_attn_narrow_kernel(TreeAttn P, int tiles) {
   constexpr int D = 64, PE = PAGE * D;
   const int lane = lane_id();
@@ -904,104 +937,37 @@ __global__ __launch_bounds__(64, NT == 1 ? 3 : 2) void tree_attn_narrow_kernel(T
     }
     const bf16* kp = kpool + (fc < 16 ? off[0] : off[1]) + ko;
 #pragma unroll
-    for (int cc = 0; cc < 4; ++cc) st.k[cc] = ld_stream16(kp + 256 * cc);
+    for (int cc = 0; cc < 4; ++cc) st.k[cc] = STREAM ? ld_stream16(kp + 256 * cc) : *reinterpret_cast<const u32x4_t*>(kp + 256 * cc);
 #pragma unroll
     for (int p = 0; p < 2; ++p)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) st.v[p][i] = ld_stream8(vpool + off[p] + vo + 512 * (i >> 1) + 128 * (i & 1));
+      for (int i = 0; i < 4; ++i) {
+        const bf16* vp = vpool + off[p] + vo + 512 * (i >> 1) + 128 * (i & 1);
+        st.v[p][i] = STREAM ? ld_stream8(vp) : *reinterpret_cast<const u32x2_t*>(vp);
+      }
   };
 
   const int parent = parent_of(P, it);
-  int node[NT], head[NT];
-  bool valid[NT];
-  Frag<bf16> qf[NT][4];
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const int c = c0 + 32 * j + fc;
-    valid[j] = c < cols;
-    node[j] = min(c / G, it.n - 1);
-    head[j] = g * G + c % G;
-    const bf16* qp = reinterpret_cast<const bf16*>(P.q) + ((int64_t)(it.t0 + node[j]) * P.hq + head[j]) * D + 8 * h;
-#pragma unroll
-    for (int cc = 0; cc < 4; ++cc) qf[j][cc].load(qp + 16 * cc);
-  }
+  Columns<NT> col;
+  col.request(P, it, g, c0);
   Step a, b;
   fetch(a, 0, 0);
   fetch(b, 1, 1);
-  const Nodes nodes = nodes_of(P, it, parent);
-  Sight sight[NT];
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    sight[j] = sight_of(P, it, nodes, node[j]);
-#pragma unroll
-    for (int cc = 0; cc < 4; ++cc) qf[j][cc].keep_if(valid[j]);
-  }
-  constexpr float WEIGHT_LIMIT = 0x1p8f;
-  bool odd = false;  // values that are not finite were dropped
-  float m_run[NT], m_sub[NT], limit[NT], l[NT];
-  f32x16 acc[2][NT];
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    m_run[j] = -INFINITY;
-    m_sub[j] = 0.f;
-    limit[j] = -INFINITY;
-    l[j] = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < 2; ++dt)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[dt][j][e] = 0.f;
-  }
+  col.start(P, it, parent);
   auto attend = [&](Step& st, int step) __attribute__((always_inline)) {
     f32x16 sc[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sc[j][e] = 0.f;
-#pragma unroll
-      for (int cc = 0; cc < 4; ++cc)
-        sc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, st.k[cc]),
-                                                        __builtin_bit_cast(bf16x8_t, qf[j][cc].v), sc[j], 0, 0, 0);
-    }
+    col.scores(sc, st.k);
     const int pg = it.pg0 + 2 * step, k0 = pg * PAGE;
     const bool edge = k0 + 2 * PAGE > it.len || (P.window > 0 && k0 < it.len + it.n - P.window) || !st.ok[0] || !st.ok[1];
-    uint32_t vis[NT];
     if (__builtin_expect(edge, 0)) {
       asm volatile("");
       if ((!st.ok[0] || (!st.ok[1] && pg + 1 < it.pg1)) && lane == 0) set_error(P.err, 1);
-      const uint32_t pages = (st.ok[0] ? 0xFFFFu : 0u) | (st.ok[1] ? 0xFFFF0000u : 0u);
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        vis[j] = valid[j] ? sight[j].keys(k0, it.len) & pages : ~0u;
-        hide(sc[j], vis[j] >> (4 * h));
-      }
+      col.mask(sc, k0, it.len, (st.ok[0] ? 0xFFFFu : 0u) | (st.ok[1] ? 0xFFFF0000u : 0u));
     }
     u32x4_t pw[NT][2];
     float sum[NT];
-    auto weights = [&]() __attribute__((always_inline)) {
-#pragma unroll
-      for (int j = 0; j < NT; ++j) sum[j] = weigh(sc[j], P.scale_log2, m_sub[j], pw[j]);
-    };
-    weights();
-    bool raise = false;
-#pragma unroll
-    for (int j = 0; j < NT; ++j) raise |= sum[j] > limit[j];
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(raise) != 0, 0)) {
-      asm volatile("");
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const uint32_t o = sum[j] > limit[j];
-        auto so = __builtin_amdgcn_permlane32_swap(o, o, false, false);
-        const float m_new = (so[0] | so[1]) ? fmaxf(m_run[j], largest(sc[j]) * P.scale_log2) : m_run[j];
-        const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[j] - m_new);
-        l[j] *= alpha;
-#pragma unroll
-        for (int dt = 0; dt < 2; ++dt) acc[dt][j] *= alpha;
-        m_run[j] = m_new;
-        m_sub[j] = m_new == -INFINITY ? 0.f : m_new;
-        limit[j] = m_new == -INFINITY ? -INFINITY : WEIGHT_LIMIT;
-      }
-      weights();
-    }
+    col.weights(sc, P.scale_log2, pw, sum);
+    col.raise(sc, P.scale_log2, pw, sum);
     u32x4_t vf[2][2];
 #pragma unroll
     for (int p = 0; p < 2; ++p)
@@ -1009,18 +975,9 @@ __global__ __launch_bounds__(64, NT == 1 ? 3 : 2) void tree_attn_narrow_kernel(T
       for (int dt = 0; dt < 2; ++dt) vf[p][dt] = __builtin_shufflevector(st.v[p][2 * dt], st.v[p][2 * dt + 1], 0, 1, 2, 3);
     if (__builtin_expect(edge, 0)) {
       asm volatile("");
-      odd |= drop_nonfinite(vf);
+      col.odd |= drop_nonfinite(vf);
     }
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      l[j] += sum[j];
-#pragma unroll
-      for (int p = 0; p < 2; ++p)
-#pragma unroll
-        for (int dt = 0; dt < 2; ++dt)
-          acc[dt][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf[p][dt]),
-                                                               __builtin_bit_cast(bf16x8_t, pw[j][p]), acc[dt][j], 0, 0, 0);
-    }
+    col.add(vf, pw, sum);
   };
   // blocks of 30 steps, whose ids and those of the two steps requested ahead sit in one register; a step past
   // the end reads the last page again and is masked
@@ -1040,27 +997,35 @@ __global__ __launch_bounds__(64, NT == 1 ? 3 : 2) void tree_attn_narrow_kernel(T
     ids = next;
   }
   if (g == 0 && tile == 0) write_rows(P, it);
-  if (odd) add_nonfinite<NT>(P, it, g, sight, valid, h, acc);
-  finish<NT>(P, it, node, head, valid, h, m_run, l, acc);
+  if (col.odd) add_nonfinite<NT>(P, it, g, col);
+  finish<NT>(P, it, col);
 }
 
 // The kernel for a step and the columns that one of its wavefronts or workgroups
 // takes. bf16 with head dim 64 has the 32 x 32 products; their loads need 16-byte
-// aligned pools. `cols` is the largest tree's node and head pairs per KV head;
-// `light`: the step's splits leave compute units idle. Measured, 64 query heads on 8
-// KV heads (us):
-//   up to 32 columns, 48 trees of 1-4 nodes behind ~4 K tokens: NARROW1 100, NARROW2 106, WIDE2 136
-//   up to 64, 48 trees of 1-8: NARROW2 114, NARROW1 171, WIDE2 150
-//   up to 128, 48 trees of 8-16: WIDE2 127, WIDE1 140, NARROW2 174; light, one tree of 16 behind 6 K: WIDE1
-//     12.8, WIDE2 14.5; 256 windowed trees of 2-12: WIDE1 37, WIDE2 39, NARROW2 40
+// aligned pools. `cols` is the largest tree's node and head pairs per KV head; `few`:
+// the step's pages fit the caches and its splits leave compute units idle; `one_each`:
+// no tree is split. Latency bounds such steps, and bandwidth or the vector pipe the
+// rest. Streaming loads serve pages that one wavefront or workgroup reads, once; with
+// several column tiles they make each fetch its pages anew. Measured in us, 64 query
+// heads on 8 KV heads, six sets of pools in turn:
+//   up to 32 columns, 256 windowed trees of 1-4 nodes: NARROW1_STREAM 20.4, NARROW1 23.8, NARROW2 21.6; 48 of 1-4
+//     behind 4-16 K tokens NARROW1_STREAM 103, NARROW1 114, NARROW2 103, WIDE2 108; one behind 6 K NARROW1 9.3,
+//     WIDE1 9.8
+//   up to 96, 256 windowed trees of 2-12: NARROW1 35, NARROW1_STREAM 36, NARROW2 40, WIDE1 40; one of 8 behind 6 K
+//     NARROW1 10.2, WIDE1 10.7, NARROW2 11.7
+//   few or one each, above: 256 windowed trees of 8-16 WIDE1 46, NARROW2 47, NARROW1 51; one of 16 behind 6 K WIDE1 11.7,
+//     NARROW1 12.1, WIDE2 14.5; of 64 WIDE1 21.3, WIDE4 22.5; 16 windowed of 17-30 WIDE1 11.8, WIDE4 16.5
+//   up to 64, 48 trees of 1-8: NARROW2 114 (126 without streaming loads), NARROW1_STREAM 171, WIDE2 150
+//   up to 128, 48 trees of 8-16: WIDE2 125, WIDE1 140, NARROW2 174
 //   above, 24 trees of 16-32: WIDE4 174, WIDE2 205; one workgroup of eight wavefronts for 512 columns was 10-20%
 //     slower than two of WIDE4, whose barriers stop fewer wavefronts
-TreeForm tree_attn_form(int dtype, int head_dim, const void* k_pool, const void* v_pool, int cols, bool light) {
+TreeForm tree_attn_form(int dtype, int head_dim, const void* k_pool, const void* v_pool, int cols, bool few, bool one_each) {
   if (dtype != 1 || head_dim != 64 || ((uintptr_t)k_pool | (uintptr_t)v_pool) % 16) return {TREE_ANY, 16, 12};
-  if (cols <= 32) return {TREE_NARROW1, 32, 8};
-  if (cols <= 64 && !light) return {TREE_NARROW2, 64, 8};
-  if (cols <= 128) return light ? TreeForm{TREE_WIDE1, 128, 3} : TreeForm{TREE_WIDE2, 128, 4};
-  return {TREE_WIDE4, 256, 2};
+  if (cols <= 32) return {few ? TREE_NARROW1 : TREE_NARROW1_STREAM, 32, 8};
+  if (few || one_each) return cols <= 96 ? TreeForm{TREE_NARROW1, 32, 8} : TreeForm{TREE_WIDE1, 128, 3};
+  if (cols <= 64) return {TREE_NARROW2, 64, 8};
+  return cols <= 128 ? TreeForm{TREE_WIDE2, 128, 4} : TreeForm{TREE_WIDE4, 256, 2};
 }
 
 hipError_t launch_tree_attn(int dtype, int head_dim, const TreeAttn& p, hipStream_t s) {
@@ -1071,8 +1036,9 @@ hipError_t launch_tree_attn(int dtype, int head_dim, const TreeAttn& p, hipStrea
   if (groups > 0x7FFFFFFF) return hipErrorInvalidValue;
   const dim3 grid((unsigned)groups);
   switch (p.form.kind) {
-    case TREE_NARROW1: hipLaunchKernelGGL(tree_attn_narrow_kernel<1>, grid, dim3(64), 0, s, p, tiles); break;
-    case TREE_NARROW2: hipLaunchKernelGGL(tree_attn_narrow_kernel<2>, grid, dim3(64), 0, s, p, tiles); break;
+    case TREE_NARROW1: hipLaunchKernelGGL((tree_attn_narrow_kernel<1, false>), grid, dim3(64), 0, s, p, tiles); break;
+    case TREE_NARROW1_STREAM: hipLaunchKernelGGL((tree_attn_narrow_kernel<1, true>), grid, dim3(64), 0, s, p, tiles); break;
+    case TREE_NARROW2: hipLaunchKernelGGL((tree_attn_narrow_kernel<2, true>), grid, dim3(64), 0, s, p, tiles); break;
     case TREE_WIDE1: hipLaunchKernelGGL((tree_attn_wide_kernel<4, 1, 6>), grid, dim3(256), 0, s, p, tiles); break;
     case TREE_WIDE2: hipLaunchKernelGGL((tree_attn_wide_kernel<2, 2, 4>), grid, dim3(128), 0, s, p, tiles); break;
     case TREE_WIDE4: hipLaunchKernelGGL((tree_attn_wide_kernel<4, 2, 6>), grid, dim3(256), 0, s, p, tiles); break;
