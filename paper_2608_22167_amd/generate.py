@@ -82,17 +82,28 @@ class Lookup:
     def __init__(self, ngram: int = 3, width: int = 2):
         self.ngram, self.width = ngram, width
         self.after: Dict[tuple, deque] = {}   # tokens -> the latest positions behind them
-        self.seen = 0
+        self.history: List[int] = []
+
+    def feed(self, tokens: Sequence[int]) -> None:
+        """The tokens that follow those fed so far."""
+        h = self.history
+        for t in tokens:
+            i = len(h)
+            for n in range(1, min(self.ngram, i) + 1):
+                self.after.setdefault(tuple(h[i - n:i]), deque(maxlen=self.width)).append(i)
+            h.append(t)
 
     def tree(self, history: Sequence[int], max_nodes: int, max_depth: int) -> Tuple[List[int], List[int]]:
-        """At most max_nodes tokens, max_depth in a row, to follow `history` (a
-        longer one than at the last call, with the same beginning); the places'
-        common beginnings are shared. Returns the tokens and their parents (index of
-        the token before, -1: the history's end)."""
-        for i in range(max(self.seen, 1), len(history)):
-            for n in range(1, min(self.ngram, i) + 1):
-                self.after.setdefault(tuple(history[i - n:i]), deque(maxlen=self.width)).append(i)
-        self.seen = len(history)
+        """`draft` behind `history`, a longer one than was fed so far, with the same
+        beginning."""
+        self.feed(history[len(self.history):])
+        return self.draft(max_nodes, max_depth)
+
+    def draft(self, max_nodes: int, max_depth: int) -> Tuple[List[int], List[int]]:
+        """At most max_nodes tokens, max_depth in a row, to follow the tokens fed; the
+        places' common beginnings are shared. Returns the tokens and their parents
+        (index of the token before, -1: the last one fed)."""
+        history = self.history
         places: Sequence[int] = ()
         for n in range(min(self.ngram, len(history)), 0, -1):
             places = self.after.get(tuple(history[-n:]), ())

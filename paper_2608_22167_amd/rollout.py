@@ -35,6 +35,7 @@ from typing import Dict, List, Optional
 import numpy as np
 
 from paper_2608_22167_amd.generate import Lookup
+from paper_2608_22167_amd.mcpu import TREE_MAX_NODES
 
 
 @dataclass
@@ -82,6 +83,8 @@ class Engine:
     tokens in fewer steps."""
 
     def __init__(self, gen, draft_nodes: int = 0):
+        if not 0 <= draft_nodes < TREE_MAX_NODES:
+            raise ValueError(f"draft_nodes {draft_nodes}: a tree has up to {TREE_MAX_NODES} nodes, one of them its root")
         self.gen = gen
         self.draft_nodes = draft_nodes
         self.lookups: Dict[int, Lookup] = {}
@@ -135,7 +138,9 @@ class Engine:
         for s in live:
             left = self.want[s.sid][0] - len(self.want[s.sid][1]) if s.sid in self.want else 1
             look = self.lookups.setdefault(s.sid, Lookup())
-            drafts[s.sid] = look.tree(s.history + s.pending, self.draft_nodes, left - 1)
+            look.feed(s.history[len(look.history):])  # the last pending token was drawn then, and is part of it
+            look.feed(s.pending[len(look.history) - len(s.history):])
+            drafts[s.sid] = look.draft(self.draft_nodes, left - 1)
         return self.gen.step_tree(drafts)
 
     def _loop(self):

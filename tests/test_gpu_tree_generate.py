@@ -114,6 +114,23 @@ def test_layer_over_trees_of_mxfp4_and_of_chains():
     assert torch.equal(a[3], b[3]) and torch.equal(a[4], b[4])  # the same keys and values, bit for bit
 
 
+@pytest.mark.parametrize("batch", [5, 20, 300])
+def test_layer_over_many_chains(batch):
+    """Up to 300 chains, whose projections take other kernels than a few rows do (and more than 256 trees)."""
+    shape = replace(W.GPT_OSS_20B, n_experts=4, top_k=4, hidden=512, ffn_dim=256, n_q_heads=16, n_kv_heads=4, window=40)
+    rng = np.random.default_rng(batch)
+    seq = rng.integers(0, 150, batch).astype(np.int32)
+    n = rng.integers(30, 65, batch) if batch < 100 else rng.integers(1, 16, batch)
+    wl = W.custom(shape, seq, n, 1305, sink_std=0.5)
+    par = np.concatenate([np.arange(-1, k - 1) for k in n]).astype(np.int32)
+    weights = mcpu.DeviceWeights(shape, wl.weights)
+    args = (wl, weights, wl.k_pool.cuda(), wl.v_pool.cuda(), seq, wl.cu_q, wl.x_in.cuda(), wl.page_table)
+    a, b = _layer(*args, par), _layer(*args)
+    for name, i in (("o", 0), ("h1", 1), ("out", 2)):
+        PT.check(name, a[i].float().cpu(), b[i].float().cpu(), "bf16")
+    assert torch.equal(a[3], b[3]) and torch.equal(a[4], b[4])
+
+
 def test_layer_over_trees_in_a_graph():
     """A captured step, replayed with other inputs in the same tensors and eager work in between."""
     shape = replace(W.GPT_OSS_20B, n_q_heads=16, n_kv_heads=2, hidden=256, ffn_dim=256, n_experts=4, top_k=2)

@@ -276,3 +276,23 @@ def test_tensors_off_the_gpu_are_refused():
     i = lambda *v: torch.tensor(v, dtype=torch.int32)  # noqa: E731
     with pytest.raises(mcpu.McpuError):
         mcpu.tree_accept(i(0, 1), i(-1), i(3), i(4), i(0), i(0), i(0), torch.zeros(256, dtype=torch.uint8))
+
+
+def test_lookup_fed_in_pieces_drafts_the_same():
+    from paper_2608_22167_amd.generate import Lookup
+    rng = np.random.default_rng(5)
+    tokens = rng.integers(0, 4, 200).tolist()
+    pieces, whole = Lookup(), Lookup()
+    at = 0
+    while at < len(tokens):
+        n = int(rng.integers(1, 9))
+        pieces.feed(tokens[at:at + n])
+        at = min(at + n, len(tokens))
+        assert pieces.draft(12, 5) == whole.tree(tokens[:at], 12, 5) == Lookup().tree(tokens[:at], 12, 5)
+
+
+def test_engine_refuses_drafts_that_no_tree_holds():
+    from paper_2608_22167_amd import rollout
+    for bad in (-1, mcpu.TREE_MAX_NODES):
+        with pytest.raises(ValueError):
+            rollout.Engine(None, draft_nodes=bad)
