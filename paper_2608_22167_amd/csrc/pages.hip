@@ -98,7 +98,8 @@ hipError_t launch_tree_commit(int dtype, int head_dim, const TreeCommit& p, hipS
 // ---------------------------------------------------------------------------
 
 // A workgroup per (pair, pool, K or V). Bound by HBM: a page is read and written
-// once.
+// once, 1500 pages of 8 KV heads in two layers in 31.9 us (6.2 TB/s read and
+// written; a large copy 4.9, this one fits the last-level cache).
 template <typename V>
 __global__ __launch_bounds__(256) void pages_copy_kernel(PagesCopy P) {
   const int i = blockIdx.x, pool = blockIdx.y;

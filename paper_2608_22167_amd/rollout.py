@@ -282,13 +282,13 @@ def run_pipeline(cfg: RolloutConfig, engine: Engine) -> dict:
                 mean_batch=float(np.mean(engine.batch_hist)) if engine.batch_hist else 0.0, **counters)
 
 
-def sweep(gen, run_workers=(24, 48, 64, 96, 120), **kw) -> List[dict]:
+def sweep(gen, run_workers=(24, 48, 64, 96, 120), draft_nodes: int = 0, **kw) -> List[dict]:
     """The per-stage concurrency sweep: acquire fixed, run workers varied,
     in-flight capacity fixed; one engine reused across the settings."""
     rows = []
     for rw in run_workers:
         cfg = RolloutConfig(run_workers=rw, **kw)
-        eng = Engine(gen)
+        eng = Engine(gen, draft_nodes)
         try:
             res = run_pipeline(cfg, eng)
         finally:
@@ -315,13 +315,14 @@ if __name__ == "__main__":  # pragma: no cover - the GPU sweep
     ap.add_argument("--turns", type=int, default=4)
     ap.add_argument("--tokens-per-turn", type=int, default=32)
     ap.add_argument("--run-workers", default="24,48,64,96,120")
+    ap.add_argument("--draft-nodes", type=int, default=0, help="tokens drafted per decode step from a sequence's history")
     args = ap.parse_args()
     torch.cuda.set_device(0)
     spec = GenSpec(n_layers=args.layers, base=W.GPT_OSS_20B, vocab=W.GPT_OSS_VOCAB, pages_full=16384, pages_sw=4096,
                    max_ctx=8192)
     gen = Generator(spec, max_tokens_per_step=8192)
-    rows = sweep(gen, run_workers=[int(x) for x in args.run_workers.split(",")], n_trajectories=args.trajectories,
-                 turns=args.turns, tokens_per_turn=args.tokens_per_turn, vocab=spec.vocab,
+    rows = sweep(gen, run_workers=[int(x) for x in args.run_workers.split(",")], draft_nodes=args.draft_nodes,
+                 n_trajectories=args.trajectories, turns=args.turns, tokens_per_turn=args.tokens_per_turn, vocab=spec.vocab,
                  prompt_tokens=(256, 1024), obs_tokens=(64, 512), acquire_s=(0.5, 1.5), tool_s=(0.5, 2.0),
                  eval_s=(0.05, 0.2))
     for r in rows:
