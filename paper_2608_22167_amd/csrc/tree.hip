@@ -320,10 +320,15 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(TreeAttn P, int tiles) {
     const T* vp;
     bool ok;
   };
-  auto fetch = [&](Page& p, int pg) {
-    int pid = uniform(ptab[min(pg, it.pg1 - 1)]);
+  // ids of a block of pages and of those requested ahead of it, lane i: page pg0 + base + i (the split's last past
+  // its end); the next block's are loaded a block ahead
+  constexpr int BLK = 60;
+  const int pages = it.pg1 - it.pg0;
+  auto ids_of = [&](int base) { return ptab[it.pg0 + min(base + lane, pages - 1)]; };
+  int ids = ids_of(0);
+  auto fetch = [&](Page& p, int at) __attribute__((always_inline)) {  // `at`: the page's place in ids
+    int pid = __builtin_amdgcn_readlane(ids, at);
     p.ok = pid >= 0 && pid < P.n_pages;
-    if (!p.ok && pg < it.pg1 && lane == 0) set_error(P.err, 1);
     pid = p.ok ? pid : 0;
     const T* kp = kpool + pid * page_elems + head_off;
     p.vp = vpool + pid * page_elems + head_off;
@@ -332,12 +337,14 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(TreeAttn P, int tiles) {
 #pragma unroll
     for (int n = 0; n < D / 16; ++n) p.v[n].load(p.vp + (64 * n + lane) * 4);
   };
-  // four pages in flight, as short contexts are latency alone (three trees over up to 512 cached tokens, fp32: 7.4 us,
-  // 9.9 with one page ahead); the first before the tree's ancestors are worked out
+  // four pages in flight, as short contexts are latency alone, the first before the tree's ancestors are worked out:
+  // three trees over up to 512 cached tokens, fp32: 6.9 us, 9.9 with one page ahead, 7.4 with eight or with page
+  // ids loaded one by one (64 trees over ~3,000: 78, 102 and 85)
   constexpr int PF = 4;
+  static_assert(BLK % PF == 0 && BLK + PF <= 64, "a block's ids and those requested ahead of it");
   Page ring[PF];
 #pragma unroll
-  for (int u = 0; u < PF; ++u) fetch(ring[u], it.pg0 + u);
+  for (int u = 0; u < PF; ++u) fetch(ring[u], u);
   const Sight sight = sight_of(P, it, nodes_of(P, it, parent), node);
   if (g == 0 && tile == 0) write_rows(P, it);
 #pragma unroll
@@ -358,6 +365,7 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(TreeAttn P, int tiles) {
     for (int r = 0; r < 4; ++r) x[r] = sc[r] * P.scale_log2;
     bool odd = false;
     if (edge) {
+      if (!cur.ok && lane == 0) set_error(P.err, 1);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const bool in = sight.key(k0 + 4 * grp + r, it.len, it.n) & cur.ok;
@@ -396,13 +404,19 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(TreeAttn P, int tiles) {
       }
     }
   };
-  for (int pg = it.pg0; pg < it.pg1; pg += PF) {
+  for (int base = 0;;) {
+    const int next = ids_of(base + BLK), stop = min(pages, base + BLK);
+    for (int i = base; i < stop; i += PF) {
 #pragma unroll
-    for (int u = 0; u < PF; ++u) {
-      if (pg + u >= it.pg1) break;
-      attend(ring[u], pg + u);
-      fetch(ring[u], pg + u + PF);
+      for (int u = 0; u < PF; ++u) {
+        if (i + u >= stop) break;
+        attend(ring[u], it.pg0 + i + u);
+        fetch(ring[u], i + u + PF - base);
+      }
     }
+    if (stop == pages) break;
+    base = stop;
+    ids = next;
   }
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
