@@ -164,15 +164,18 @@ def _buf(t, n, dtype=torch.int32) -> int:
     return t.data_ptr()
 
 
+_addressof, _view = ctypes.addressof, ctypes.c_char.from_buffer
+
+
 def _host(a: np.ndarray) -> int:
     """Address of a contiguous host array."""
-    return ctypes.addressof(ctypes.c_char.from_buffer(a)) if a.size and a.flags.writeable else a.ctypes.data
+    return _addressof(_view(a)) if a.size and a.flags.writeable else a.ctypes.data
 
 
 def _stream_on(t, stream=None) -> int:
     """The stream to launch on: `stream`, or the current one; the tensors have to live on the current device."""
-    dev = t.get_device()
-    if dev != torch.cuda.current_device():
+    dev = t.get_device()  # of a tensor on the GPU, so that torch has set up its devices
+    if dev < 0 or dev != torch._C._cuda_getDevice():
         raise McpuError(MCPU_EINVAL, f"tensors on device {dev}, current device {torch.cuda.current_device()}")
     return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(dev)
 
@@ -383,7 +386,7 @@ def _tree_batch(page_table, host_seq_lens, host_cu_q):
 def tree_attention(shape, sinks, pool: KVPool, page_table, seq_lens, cu_q, parents, host_seq_lens, host_cu_q,
                    q, o, workspace, stream=None):
     hs, hc, batch, max_pages = _tree_batch(page_table, host_seq_lens, host_cu_q)
-    n, width, dt = int(hc[batch]), shape.n_q_heads * shape.head_dim, shape.torch_dtype
+    n, width, dt = hc.item(batch), shape.n_q_heads * shape.head_dim, shape.torch_dtype
     _check(lib().tree_attention(_cfg_for(shape, pool), _ptr(sinks), pool.handle, batch,
                                 _buf(page_table, batch * max_pages), max_pages, _buf(seq_lens, batch),
                                 _buf(cu_q, batch + 1), _buf(parents, n), _host(hs), _host(hc), _buf(q, n * width, dt),
@@ -447,7 +450,7 @@ def decode_layer_tree(shape, weights: DeviceWeights, pool: KVPool, page_table, s
                       workspace=None, stream=None):
     """decode_layer where each sequence's new tokens are a tree of drafted tokens."""
     hs, hc, batch, max_pages = _tree_batch(page_table, host_seq_lens, host_cu_q)
-    n = int(hc[batch])
+    n = hc.item(batch)
     _check(lib().decode_layer_tree(_cfg_for(shape, pool), ctypes.byref(weights.struct), pool.handle, batch,
                                    _buf(page_table, batch * max_pages), max_pages, _buf(seq_lens, batch),
                                    _buf(cu_q, batch + 1), _buf(parents, n), _host(hs), _host(hc),
