@@ -458,9 +458,10 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(TreeAttn P, int tiles) {
 // The maximum of a column is raised only when a lane's share of a step's weights
 // would pass 2^8, so that most steps have no cross-lane step and no rescale.
 //
-// Bound by the vector pipe on wide trees: 16 trees of 33-64 nodes behind 8-16 K tokens
-// take 200 us (630 TFLOP/s over the pairs in sight), 174 with the loads taken out; on
-// narrow ones by HBM.
+// Wide trees are bound by the vector pipe beside the products: 16 trees of 33-64 nodes
+// behind 8-16 K tokens take 196 us with the combine (640 TFLOP/s over the pairs in
+// sight); without loads and barriers the same instructions take 85% of that. Narrow
+// trees are bound by HBM.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) void* lds_void_t;
@@ -595,47 +596,38 @@ struct Columns {
       hide(t[j], vis >> (4 * (lane_id() >> 5)));
     }
   }
-  __device__ __forceinline__ void weights(const f32x16 (&t)[NT], float scale_log2, u32x4_t (&pw)[NT][2], float (&sum)[NT]) const {
-#pragma unroll
-    for (int j = 0; j < NT; ++j) sum[j] = weigh(t[j], scale_log2, m_sub[j], pw[j]);
+  // tile j's weights of a step, packed, and their sum
+  __device__ __forceinline__ float weights(int j, const f32x16& t, float scale_log2, u32x4_t (&pw)[2]) const {
+    return weigh(t, scale_log2, m_sub[j], pw);
   }
   // The maximum only has to keep the weights in range, so it is raised when a step's sum says that they are not, and
   // until a column has seen a key; the weights are then formed again.
-  __device__ __forceinline__ void raise(const f32x16 (&t)[NT], float scale_log2, u32x4_t (&pw)[NT][2], float (&sum)[NT]) {
-    bool any = false;
-#pragma unroll
-    for (int j = 0; j < NT; ++j) any |= sum[j] > limit[j];
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(any) != 0, 0)) {  // wave-uniform; the empty asm keeps it a branch
+  __device__ __forceinline__ void raise(int j, const f32x16& t, float scale_log2, u32x4_t (&pw)[2], float& sum) {
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(sum > limit[j]) != 0, 0)) {  // wave-uniform; the empty asm keeps it a branch
       asm volatile("");
+      // a column's own lanes decide, so that its bits do not depend on the columns beside it
+      const uint32_t o = sum > limit[j];
+      auto so = __builtin_amdgcn_permlane32_swap(o, o, false, false);
+      const float m_new = (so[0] | so[1]) ? fmaxf(m_run[j], largest(t) * scale_log2) : m_run[j];
+      const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[j] - m_new);
+      l[j] *= alpha;
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        // a column's own lanes decide, so that its bits do not depend on the columns beside it
-        const uint32_t o = sum[j] > limit[j];
-        auto so = __builtin_amdgcn_permlane32_swap(o, o, false, false);
-        const float m_new = (so[0] | so[1]) ? fmaxf(m_run[j], largest(t[j]) * scale_log2) : m_run[j];
-        const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[j] - m_new);
-        l[j] *= alpha;
-#pragma unroll
-        for (int dt = 0; dt < 2; ++dt) acc[dt][j] *= alpha;
-        m_run[j] = m_new;
-        m_sub[j] = m_new == -INFINITY ? 0.f : m_new;  // masked scores give 2^-inf = 0
-        limit[j] = m_new == -INFINITY ? -INFINITY : WEIGHT_LIMIT;
-      }
-      weights(t, scale_log2, pw, sum);
+      for (int dt = 0; dt < 2; ++dt) acc[dt][j] *= alpha;
+      m_run[j] = m_new;
+      m_sub[j] = m_new == -INFINITY ? 0.f : m_new;  // masked scores give 2^-inf = 0
+      limit[j] = m_new == -INFINITY ? -INFINITY : WEIGHT_LIMIT;
+      sum = weights(j, t, scale_log2, pw);
     }
   }
-  // O^T += V^T P^T
-  __device__ __forceinline__ void add(const u32x4_t (&vf)[2][2], const u32x4_t (&pw)[NT][2], const float (&sum)[NT]) {
+  // O^T += V^T P^T of tile j
+  __device__ __forceinline__ void add(int j, const u32x4_t (&vf)[2][2], const u32x4_t (&pw)[2], float sum) {
+    l[j] += sum;
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      l[j] += sum[j];
+    for (int p = 0; p < 2; ++p)
 #pragma unroll
-      for (int p = 0; p < 2; ++p)
-#pragma unroll
-        for (int dt = 0; dt < 2; ++dt)
-          acc[dt][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf[p][dt]),
-                                                               __builtin_bit_cast(bf16x8_t, pw[j][p]), acc[dt][j], 0, 0, 0);
-    }
+      for (int dt = 0; dt < 2; ++dt)
+        acc[dt][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf[p][dt]),
+                                                             __builtin_bit_cast(bf16x8_t, pw[p]), acc[dt][j], 0, 0, 0);
   }
 };
 // The steps with masked keys once more, for values that are not finite: added to the
@@ -736,19 +728,6 @@ __device__ __forceinline__ void attend_stage(const TreeAttn& P, const TreeItem& 
     if ((!ok[0] || (!ok[1] && second)) && lane == 0) set_error(P.err, 1);
     col.mask(sc, k0, it.len, (ok[0] ? 0xFFFFu : 0u) | (ok[1] && second ? 0xFFFF0000u : 0u));
   }
-  u32x4_t pw[NT][2];  // [column tile][page]: the weights, packed
-  float sum[NT];
-  __builtin_amdgcn_sched_barrier(0);
-  col.scores(sn, kf);
-  col.weights(sc, P.scale_log2, pw, sum);
-  // the next scores' products among the vector instructions of the weights, 12 each
-#define TREE_MIX                                      \
-  __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  \
-  __builtin_amdgcn_sched_group_barrier(0x402, 12, 0);
-  TREE_MIX TREE_MIX TREE_MIX TREE_MIX
-  if constexpr (NT == 2) { TREE_MIX TREE_MIX TREE_MIX TREE_MIX }
-#undef TREE_MIX
-  col.raise(sc, P.scale_log2, pw, sum);
   // dim l % 32 of a tile of 32, value rows 4 h .. and 8 + 4 h ..
   const uint32_t vbase = (fc >> 4) * 512 + (fc & 15) * 8 + (((uint32_t)h ^ ((fc >> 4) & 1)) << 7);
   u32x4_t vf[2][2];  // [page][dim tile]
@@ -760,11 +739,35 @@ __device__ __forceinline__ void attend_stage(const TreeAttn& P, const TreeItem& 
       const u32x2_t a = *reinterpret_cast<const u32x2_t*>(v), c = *reinterpret_cast<const u32x2_t*>(v + 256);
       vf[p][dt] = __builtin_shufflevector(a, c, 0, 1, 2, 3);
     }
+  u32x4_t pw[NT][2];  // [column tile][page]: the weights, packed
+  float sum[NT];
+  // the next scores' products among the vector instructions of the first tile's weights, the first tile's value
+  // products among those of the second's (24 trees of 16-32: 140 us, 146 with all weights before all value products)
+  __builtin_amdgcn_sched_barrier(0);
+  col.scores(sn, kf);
+  sum[0] = col.weights(0, sc[0], P.scale_log2, pw[0]);
+#pragma unroll
+  for (int i = 0; i < 4 * NT; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x402, NT == 2 ? 6 : 12, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+  }
+  col.raise(0, sc[0], P.scale_log2, pw[0], sum[0]);
   if (__builtin_expect(edge, 0)) {
     asm volatile("");
     col.odd |= drop_nonfinite(vf);
   }
-  col.add(vf, pw, sum);
+  if constexpr (NT == 2) {
+    __builtin_amdgcn_sched_barrier(0);
+    col.add(0, vf, pw[0], sum[0]);
+    sum[1] = col.weights(1, sc[1], P.scale_log2, pw[1]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x402, 12, 0);
+    }
+    col.raise(1, sc[1], P.scale_log2, pw[1], sum[1]);
+  }
+  col.add(NT - 1, vf, pw[NT - 1], sum[NT - 1]);
 }
 // Piece w of a step, 1 KB, into its stage: half w % 2 of K of page 0, K of page 1, V
 // of page 0, V of page 1 (w / 2) of pool page `id`; a `range` of 0 touches no memory.
@@ -986,8 +989,11 @@ __global__ __launch_bounds__(64, NT == 1 ? 3 : 2) void tree_attn_narrow_kernel(T
     }
     u32x4_t pw[NT][2];
     float sum[NT];
-    col.weights(sc, P.scale_log2, pw, sum);
-    col.raise(sc, P.scale_log2, pw, sum);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      sum[j] = col.weights(j, sc[j], P.scale_log2, pw[j]);
+      col.raise(j, sc[j], P.scale_log2, pw[j], sum[j]);
+    }
     u32x4_t vf[2][2];
 #pragma unroll
     for (int p = 0; p < 2; ++p)
@@ -997,7 +1003,8 @@ __global__ __launch_bounds__(64, NT == 1 ? 3 : 2) void tree_attn_narrow_kernel(T
       asm volatile("");
       col.odd |= drop_nonfinite(vf);
     }
-    col.add(vf, pw, sum);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) col.add(j, vf, pw[j], sum[j]);
   };
   // blocks of 30 steps, whose ids and those of the two steps requested ahead sit in one register; a step past
   // the end reads the last page again and is masked
