@@ -34,7 +34,7 @@ hipError_t launch_tree_plan(const TreeArgs& p, TreeItem* out, hipStream_t s);
 // How a step's columns (node and query head pairs of one KV head) are dealt out:
 // `cols` of them to each workgroup (each wavefront for TREE_ANY), of which `per_cu`
 // are at work on a compute unit at a time.
-enum TreeKind { TREE_ANY, TREE_NARROW1, TREE_NARROW1_STREAM, TREE_NARROW2, TREE_WIDE1, TREE_WIDE2, TREE_WIDE4 };
+enum TreeKind { TREE_ANY, TREE_NARROW, TREE_NARROW_STREAM, TREE_WIDE1, TREE_WIDE2, TREE_WIDE4 };
 struct TreeForm {
   int kind, cols, per_cu;
 };

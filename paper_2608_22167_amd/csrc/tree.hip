@@ -913,14 +913,14 @@ __global__ __launch_bounds__(64 * NC, NT == 1 ? 4 : 2) void tree_attn_wide_kerne
   finish<NT>(P, it, col);
 }
 
-// The same products for few columns: one wavefront per split, KV head and NT x 32
-// columns, its pages straight to registers, two steps in flight. Nothing is shared,
+// The same products for few columns: one wavefront per split, KV head and 32 columns,
+// its pages straight to registers, two steps in flight. Nothing is shared,
 // so there is no LDS and no barrier, and the wavefronts of a SIMD hide each other's
-// loads and products. Bound by HBM on large batches (48 trees of 1-8 nodes behind ~4 K
-// tokens: 92 us, 5.5 TB/s; the loads alone 91), by the latency of row offsets, page
-// ids and pages one after the other on small ones (one tree of 4 behind 6 K: 9.3 us).
-template <int NT, bool STREAM>
-__global__ __launch_bounds__(64, NT == 1 ? 3 : 2) void tree_attn_narrow_kernel(TreeAttn P, int tiles) {
+// loads and products. Bound by HBM on large batches (48 trees of 1-4 nodes behind 4-16 K
+// tokens: 102 us, 5.7 TB/s), by the latency of row offsets, page ids and pages one
+// after the other on small ones (one tree of 4 behind 6 K: 8.9 us).
+template <bool STREAM>
+__global__ __launch_bounds__(64, 3) void tree_attn_narrow_kernel(TreeAttn P, int tiles) {
   constexpr int D = 64, PE = PAGE * D;
   const int lane = lane_id();
   const unsigned hkv = P.hkv, slot = blockIdx.x >> 3;
@@ -929,7 +929,7 @@ __global__ __launch_bounds__(64, NT == 1 ? 3 : 2) void tree_attn_narrow_kernel(T
   if (item >= P.n_items) return;
   TreeItem it;
   if (!find_item(P, item, it)) return;
-  const int G = P.hq / P.hkv, cols = it.n * G, c0 = 32 * NT * tile;
+  const int G = P.hq / P.hkv, cols = it.n * G, c0 = 32 * tile;
   if (c0 >= cols) return;
   const int32_t* ptab = P.page_table + (int64_t)it.b * P.max_pages;
   const int n_steps = (it.pg1 - it.pg0 + 1) / 2;
@@ -971,14 +971,14 @@ __global__ __launch_bounds__(64, NT == 1 ? 3 : 2) void tree_attn_narrow_kernel(T
   };
 
   const int parent = parent_of(P, it);
-  Columns<NT> col;
+  Columns<1> col;
   col.request(P, it, g, c0);
   Step a, b;
   fetch(a, 0, 0);
   fetch(b, 1, 1);
   col.start(P, it, parent);
   auto attend = [&](Step& st, int step) __attribute__((always_inline)) {
-    f32x16 sc[NT];
+    f32x16 sc[1];
     col.scores(sc, st.k);
     const int pg = it.pg0 + 2 * step, k0 = pg * PAGE;
     const bool edge = k0 + 2 * PAGE > it.len || (P.window > 0 && k0 < it.len + it.n - P.window) || !st.ok[0] || !st.ok[1];
@@ -987,13 +987,9 @@ __global__ __launch_bounds__(64, NT == 1 ? 3 : 2) void tree_attn_narrow_kernel(T
       if ((!st.ok[0] || (!st.ok[1] && pg + 1 < it.pg1)) && lane == 0) set_error(P.err, 1);
       col.mask(sc, k0, it.len, (st.ok[0] ? 0xFFFFu : 0u) | (st.ok[1] ? 0xFFFF0000u : 0u));
     }
-    u32x4_t pw[NT][2];
-    float sum[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      sum[j] = col.weights(j, sc[j], P.scale_log2, pw[j]);
-      col.raise(j, sc[j], P.scale_log2, pw[j], sum[j]);
-    }
+    u32x4_t pw[2];
+    float sum = col.weights(0, sc[0], P.scale_log2, pw);
+    col.raise(0, sc[0], P.scale_log2, pw, sum);
     u32x4_t vf[2][2];
 #pragma unroll
     for (int p = 0; p < 2; ++p)
@@ -1003,8 +999,7 @@ __global__ __launch_bounds__(64, NT == 1 ? 3 : 2) void tree_attn_narrow_kernel(T
       asm volatile("");
       col.odd |= drop_nonfinite(vf);
     }
-#pragma unroll
-    for (int j = 0; j < NT; ++j) col.add(j, vf, pw[j], sum[j]);
+    col.add(0, vf, pw, sum);
   };
   // blocks of 30 steps, whose ids and those of the two steps requested ahead sit in one register; a step past
   // the end reads the last page again and is masked
@@ -1024,8 +1019,8 @@ __global__ __launch_bounds__(64, NT == 1 ? 3 : 2) void tree_attn_narrow_kernel(T
     ids = next;
   }
   if (g == 0 && tile == 0) write_rows(P, it);
-  if (col.odd) add_nonfinite<NT>(P, it, g, col);
-  finish<NT>(P, it, col);
+  if (col.odd) add_nonfinite<1>(P, it, g, col);
+  finish<1>(P, it, col);
 }
 
 // The kernel for a step and the columns that one of its wavefronts or workgroups
@@ -1035,23 +1030,25 @@ __global__ __launch_bounds__(64, NT == 1 ? 3 : 2) void tree_attn_narrow_kernel(T
 // no tree is split. Latency bounds such steps, and bandwidth or the vector pipe the
 // rest. Streaming loads serve pages that one wavefront or workgroup reads, once; with
 // several column tiles they make each fetch its pages anew. Measured in us, 64 query
-// heads on 8 KV heads, six sets of pools in turn:
-//   up to 32 columns, 256 windowed trees of 1-4 nodes: NARROW1_STREAM 20.4, NARROW1 23.8, NARROW2 21.6; 48 of 1-4
-//     behind 4-16 K tokens NARROW1_STREAM 103, NARROW1 114, NARROW2 103, WIDE2 108; one behind 6 K NARROW1 9.3,
-//     WIDE1 9.8
-//   up to 96, 256 windowed trees of 2-12: NARROW1 35, NARROW1_STREAM 36, NARROW2 40, WIDE1 40; one of 8 behind 6 K
-//     NARROW1 10.2, WIDE1 10.7, NARROW2 11.7
-//   few or one each, above: 256 windowed trees of 8-16 WIDE1 46, NARROW2 47, NARROW1 51; one of 16 behind 6 K WIDE1 11.7,
-//     NARROW1 12.1, WIDE2 14.5; of 64 WIDE1 21.3, WIDE4 22.5; 16 windowed of 17-30 WIDE1 11.8, WIDE4 16.5
-//   up to 64, 48 trees of 1-8: NARROW2 114 (126 without streaming loads), NARROW1_STREAM 171, WIDE2 150
-//   up to 128, 48 trees of 8-16: WIDE2 125, WIDE1 140, NARROW2 174
-//   above, 24 trees of 16-32: WIDE4 174, WIDE2 205; one workgroup of eight wavefronts for 512 columns was 10-20%
-//     slower than two of WIDE4, whose barriers stop fewer wavefronts
+// heads on 8 KV heads, six sets of pools in turn (contexts of 4-16 K tokens unless
+// given; NARROW2 was NARROW_STREAM with two column tiles a wavefront):
+//   up to 32 columns, 256 windowed trees of 1-4 nodes: NARROW_STREAM 20.3, NARROW 23.8; 48 trees of 1-4
+//     NARROW_STREAM 102, NARROW 115, WIDE2 107; one tree of 4 behind 6 K NARROW 8.9, WIDE1 9.6
+//   few or one each, up to 96: 256 windowed trees of 2-12 NARROW 35, NARROW_STREAM 36, WIDE1 and WIDE2 39; one
+//     tree of 8 behind 6 K NARROW 9.8, WIDE1 10.5
+//   few or one each, above: 256 windowed trees of 8-16 WIDE1 45, WIDE2 47, NARROW 50; one tree of 16 behind 6 K
+//     WIDE1 11.8, NARROW 12.0, WIDE2 13.8, of 64 WIDE1 21.6, NARROW 22.2, WIDE4 23.2; 16 windowed trees of 17-30
+//     WIDE1 12.2, WIDE4 16.0
+//   up to 128, 48 trees of 1-8: WIDE2 113 + 5 for the combine, NARROW2 108 + 9, NARROW 162; 128 trees of 1-8 WIDE2
+//     311 + 9, NARROW2 303 + 13; 24 trees of 1-8 WIDE2 50 + 6, NARROW2 53 + 8; 48 trees of 8-16 WIDE2 121, WIDE1 128,
+//     WIDE4 162
+//   above, 24 trees of 16-32: WIDE4 137, WIDE1 144, WIDE2 152; 16 of 33-64 behind 8-16 K WIDE4 164, WIDE1 164 and 3
+//     more in the combine, WIDE2 185; one workgroup of eight wavefronts for 512 columns was 10-20% slower than two of
+//     WIDE4, whose barriers stop fewer wavefronts
 TreeForm tree_attn_form(int dtype, int head_dim, const void* k_pool, const void* v_pool, int cols, bool few, bool one_each) {
   if (dtype != 1 || head_dim != 64 || ((uintptr_t)k_pool | (uintptr_t)v_pool) % 16) return {TREE_ANY, 16, 12};
-  if (cols <= 32) return {few ? TREE_NARROW1 : TREE_NARROW1_STREAM, 32, 8};
-  if (few || one_each) return cols <= 96 ? TreeForm{TREE_NARROW1, 32, 8} : TreeForm{TREE_WIDE1, 128, 3};
-  if (cols <= 64) return {TREE_NARROW2, 64, 8};
+  if (cols <= 32) return {few ? TREE_NARROW : TREE_NARROW_STREAM, 32, 8};
+  if (few || one_each) return cols <= 96 ? TreeForm{TREE_NARROW, 32, 8} : TreeForm{TREE_WIDE1, 128, 3};
   return cols <= 128 ? TreeForm{TREE_WIDE2, 128, 4} : TreeForm{TREE_WIDE4, 256, 2};
 }
 
@@ -1063,9 +1060,8 @@ hipError_t launch_tree_attn(int dtype, int head_dim, const TreeAttn& p, hipStrea
   if (groups > 0x7FFFFFFF) return hipErrorInvalidValue;
   const dim3 grid((unsigned)groups);
   switch (p.form.kind) {
-    case TREE_NARROW1: hipLaunchKernelGGL((tree_attn_narrow_kernel<1, false>), grid, dim3(64), 0, s, p, tiles); break;
-    case TREE_NARROW1_STREAM: hipLaunchKernelGGL((tree_attn_narrow_kernel<1, true>), grid, dim3(64), 0, s, p, tiles); break;
-    case TREE_NARROW2: hipLaunchKernelGGL((tree_attn_narrow_kernel<2, true>), grid, dim3(64), 0, s, p, tiles); break;
+    case TREE_NARROW: hipLaunchKernelGGL((tree_attn_narrow_kernel<false>), grid, dim3(64), 0, s, p, tiles); break;
+    case TREE_NARROW_STREAM: hipLaunchKernelGGL((tree_attn_narrow_kernel<true>), grid, dim3(64), 0, s, p, tiles); break;
     case TREE_WIDE1: hipLaunchKernelGGL((tree_attn_wide_kernel<4, 1, 6>), grid, dim3(256), 0, s, p, tiles); break;
     case TREE_WIDE2: hipLaunchKernelGGL((tree_attn_wide_kernel<2, 2, 4>), grid, dim3(128), 0, s, p, tiles); break;
     case TREE_WIDE4: hipLaunchKernelGGL((tree_attn_wide_kernel<4, 2, 6>), grid, dim3(256), 0, s, p, tiles); break;

@@ -235,7 +235,7 @@ def test_attention_on_another_stream_and_used_workspace():
 
 
 # Many KV heads make a batch large (more than 12288 (page, head) pairs) at a length that the 64-bit definition can
-# follow: 2 x 20 columns take the two-column-pair form without a stage, 2 x 50 and 4 x 40 the staged ones.
+# follow: 2 x 20 to 4 x 40 columns take the staged forms of large batches, 3 the streaming one without stages.
 @pytest.mark.parametrize("layout,n", [((64, 32, 64, "bf16"), 20), ((64, 32, 64, "bf16"), 50), ((128, 32, 64, "bf16"), 40),
                                       ((32, 32, 64, "bf16"), 3)], ids=str)
 @pytest.mark.parametrize("window", [0, 2000])
