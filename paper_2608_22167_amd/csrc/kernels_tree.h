@@ -65,6 +65,7 @@ struct TreeCombine {
   const int4* tok;
   const float* sinks;
   int n_tokens, n_rows, hq;
+  int max_splits;  // of a tree
   void* o;
 };
 hipError_t launch_tree_combine(int dtype, int head_dim, const TreeCombine& p, hipStream_t s);

@@ -460,7 +460,7 @@ constexpr int TREE_START_PAGES = 32;   // what starting and ending a split costs
 
 struct TreePlanHost {
   int n_tokens = 0, max_nodes = 0, max_len = 0;
-  int pps = 1, n_items = 0, n_rows = 0;
+  int pps = 1, n_items = 0, n_rows = 0, max_splits = 1;
   TreeForm form{};
 };
 
@@ -534,6 +534,7 @@ int plan_tree(const mcpu_layer_cfg* c, const mcpu_kv_pool* pool, int batch, int 
   out->pps = (int)pps;
   out->n_items = rows == 0 ? batch : (int)items;
   out->n_rows = (int)rows;
+  out->max_splits = (int)((longest + pps - 1) / pps);
   return MCPU_OK;
 }
 
@@ -585,7 +586,7 @@ int run_tree_attention(const mcpu_layer_cfg* c, const float* sinks, mcpu_kv_pool
   if (ph.n_rows == 0) return MCPU_OK;
   TreeCombine cb{};
   cb.part_ml = tb.part_ml; cb.part_acc = tb.part_acc; cb.tok = tb.tok; cb.sinks = sinks; cb.n_tokens = ph.n_tokens;
-  cb.n_rows = ph.n_rows; cb.hq = c->n_q_heads; cb.o = o;
+  cb.n_rows = ph.n_rows; cb.max_splits = ph.max_splits; cb.hq = c->n_q_heads; cb.o = o;
   Timed tm(MCPU_KERNEL_TREE_COMBINE, st);
   HIP_TRY(launch_tree_combine(c->dtype, c->head_dim, cb, st));
   return MCPU_OK;

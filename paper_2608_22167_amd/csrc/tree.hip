@@ -1083,19 +1083,21 @@ hipError_t launch_tree_attn(int dtype, int head_dim, const TreeAttn& p, hipStrea
 // combine: o_h = sum_s 2^(m_s - M) acc_s / (2^(sink_h log2e - M) + sum_s 2^(m_s - M) l_s)
 // ---------------------------------------------------------------------------
 
-// A wavefront per (node, head) of the trees with several splits, D / 4 lanes per
-// partial row: 256 / D rows per load, lane groups joined at the end. Bound by three
-// rounds of latency (one tree 4.8 us) and then by HBM: 16 trees of 33-64 nodes 16.7 us,
-// 20.6 with 16 rows always in flight, most of them past the last split.
-template <typename T, int D>
+// D / 4 lanes per partial row of a (node, head) of the trees with several splits: a
+// lane group per pair, which goes through its splits four at a time, or, with many
+// splits or few pairs (MANY), the whole wavefront, its lane groups joined at the end.
+// Bound by three rounds of latency, then by HBM: 31 splits of one tree 4.8 us (MANY); up
+// to four splits of 16 trees of 33-64 nodes 7.4 us (MANY 12.2, more than half of it
+// vector work of the joins), of 48 trees of 1-8 5.5 (MANY 5.1).
+template <typename T, int D, bool MANY>
 __global__ __launch_bounds__(256) void tree_combine_kernel(TreeCombine P) {
-  constexpr int LR = D / 4, RW = 64 / LR;
+  constexpr int LR = D / 4, RW = 64 / LR, STEP = MANY ? RW : 1;
   const int lane = lane_id(), sub = lane / LR, dim = 4 * (lane % LR);
-  const unsigned id = blockIdx.x * 4 + uniform(threadIdx.x >> 6), hq = P.hq;
+  const unsigned wave = blockIdx.x * 4 + uniform(threadIdx.x >> 6), id = MANY ? wave : wave * RW + sub, hq = P.hq;
   const int t = id / hq, h = id % hq;
   if (t >= P.n_tokens) return;
   const int4 tok = P.tok[t];
-  const int row0 = uniform(tok.x), n = uniform(tok.y), splits = uniform(tok.z);
+  const int row0 = tok.x, n = tok.y, splits = MANY ? uniform(tok.z) : tok.z;
   // a stale record (device arrays that disagree with the plan) stays inside the partial rows
   if (splits <= 1 || row0 < 0 || n <= 0 || n > TREE_MAX_NODES || (int64_t)row0 + (int64_t)(splits - 1) * n >= P.n_rows) return;
   const float sink = P.sinks ? P.sinks[h] * LOG2E : 0.f;
@@ -1104,12 +1106,12 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeCombine P) {
   // U rows in flight per lane
   auto join = [&](auto U_) __attribute__((always_inline)) {
     constexpr int U = decltype(U_)::value;
-    for (int k0 = sub; k0 < splits; k0 += U * RW) {
+    for (int k0 = MANY ? sub : 0; k0 < splits; k0 += U * STEP) {
       float2 ml[U];
       float4 v[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {  // past the end: the last split again, with no weight
-        const int k = k0 + u * RW;
+        const int k = k0 + u * STEP;
         const int64_t row = (int64_t)(row0 + min(k, splits - 1) * n) * P.hq + h;
         ml[u] = *reinterpret_cast<const float2*>(P.part_ml + 2 * row);
         v[u] = *reinterpret_cast<const float4*>(P.part_acc + row * D + dim);
@@ -1123,7 +1125,7 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeCombine P) {
       a.x *= r; a.y *= r; a.z *= r; a.w *= r;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const bool in = k0 + u * RW < splits;  // a row that is not finite keeps its weight
+        const bool in = k0 + u * STEP < splits;  // a row that is not finite keeps its weight
         const float f = in ? __builtin_amdgcn_exp2f(ml[u].x - base) : 0.f;
         L += in ? ml[u].y * f : 0.f;
         a.x += in ? v[u].x * f : 0.f; a.y += in ? v[u].y * f : 0.f;
@@ -1132,43 +1134,48 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeCombine P) {
       M = Mn;
     }
   };
-  if (splits <= RW) join(std::integral_constant<int, 1>{});
+  if (!MANY) join(std::integral_constant<int, 4>{});
   else if (splits <= 2 * RW) join(std::integral_constant<int, 2>{});
   else join(std::integral_constant<int, 8>{});
   // join the lane groups, then the sink
   float Mt = M;
+  if (MANY)
 #pragma unroll
-  for (int o = LR; o < 64; o <<= 1) Mt = fmaxf(Mt, __shfl_xor(Mt, o, 64));
+    for (int o = LR; o < 64; o <<= 1) Mt = fmaxf(Mt, __shfl_xor(Mt, o, 64));
   if (P.sinks) Mt = fmaxf(Mt, sink);
   const float f = __builtin_amdgcn_exp2f(M - (Mt == -INFINITY ? 0.f : Mt));
   L *= f;
   a.x *= f; a.y *= f; a.z *= f; a.w *= f;
+  if (MANY)
 #pragma unroll
-  for (int o = LR; o < 64; o <<= 1) {
-    L += __shfl_xor(L, o, 64);
-    a.x += __shfl_xor(a.x, o, 64);
-    a.y += __shfl_xor(a.y, o, 64);
-    a.z += __shfl_xor(a.z, o, 64);
-    a.w += __shfl_xor(a.w, o, 64);
-  }
+    for (int o = LR; o < 64; o <<= 1) {
+      L += __shfl_xor(L, o, 64);
+      a.x += __shfl_xor(a.x, o, 64);
+      a.y += __shfl_xor(a.y, o, 64);
+      a.z += __shfl_xor(a.z, o, 64);
+      a.w += __shfl_xor(a.w, o, 64);
+    }
   if (P.sinks) L += __builtin_amdgcn_exp2f(sink - Mt);
-  if (sub != 0) return;
+  if (MANY && sub != 0) return;
   const float inv = L == 0.f ? 0.f : 1.0f / L;
   store4(reinterpret_cast<T*>(P.o) + ((int64_t)t * P.hq + h) * D + dim,
          make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
 }
 
+template <typename T, int D>
+static void combine_impl(const TreeCombine& p, hipStream_t s) {
+  const int64_t pairs = (int64_t)p.n_tokens * p.hq;
+  constexpr int per_block = 4 * (256 / D);  // a lane group each
+  // eight splits in two rounds of loads; pairs for up to two rounds of wavefronts on the whole GPU
+  if (p.max_splits > 8 || pairs <= 16384) hipLaunchKernelGGL((tree_combine_kernel<T, D, true>), dim3((unsigned)((pairs + 3) / 4)), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((tree_combine_kernel<T, D, false>), dim3((unsigned)((pairs + per_block - 1) / per_block)), dim3(256), 0, s, p);
+}
+
 hipError_t launch_tree_combine(int dtype, int head_dim, const TreeCombine& p, hipStream_t s) {
   if (p.n_rows == 0) return hipSuccess;
   if ((int64_t)p.n_tokens * p.hq > 0x7FFFFFFF) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)(((int64_t)p.n_tokens * p.hq + 3) / 4)), block(256);
-  if (dtype == 0) {
-    if (head_dim == 32) hipLaunchKernelGGL((tree_combine_kernel<float, 32>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((tree_combine_kernel<float, 64>), grid, block, 0, s, p);
-  } else {
-    if (head_dim == 32) hipLaunchKernelGGL((tree_combine_kernel<bf16, 32>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((tree_combine_kernel<bf16, 64>), grid, block, 0, s, p);
-  }
+  if (dtype == 0) head_dim == 32 ? combine_impl<float, 32>(p, s) : combine_impl<float, 64>(p, s);
+  else head_dim == 32 ? combine_impl<bf16, 32>(p, s) : combine_impl<bf16, 64>(p, s);
   return hipGetLastError();
 }
 

@@ -237,11 +237,19 @@ def test_attention_on_another_stream_and_used_workspace():
 # Many KV heads make a batch large (more than 12288 (page, head) pairs) at a length that the 64-bit definition can
 # follow: 2 x 20 to 4 x 40 columns take the staged forms of large batches, 3 the streaming one without stages.
 @pytest.mark.parametrize("layout,n", [((64, 32, 64, "bf16"), 20), ((64, 32, 64, "bf16"), 50), ((128, 32, 64, "bf16"), 40),
+                                      ((128, 32, 64, "bf16"), 64),
                                       ((32, 32, 64, "bf16"), 3)], ids=str)
 @pytest.mark.parametrize("window", [0, 2000])
 def test_attention_of_large_batches(layout, n, window):
     rng = np.random.default_rng(n)
     Case(layout, [2500, 2481, 2500 if window else 1300, 0], trees(rng, [n, n - 1, n, 1]), window, 26).check()
+
+
+@pytest.mark.parametrize("layout", [(64, 4, 32, "f32"), (64, 4, 64, "f32"), (64, 4, 32, "bf16"), (64, 4, 64, "bf16")], ids=str)
+def test_attention_of_many_rows_in_few_splits(layout):
+    """More than 16384 (node, head) pairs in two to four splits, and a tree that is not split."""
+    rng = np.random.default_rng(33)
+    Case(layout, [600, 431, 900, 20, 750], trees(rng, [64, 60, 61, 62, 64]), 0, 34).check()
 
 
 @pytest.mark.parametrize("layout", [LAYOUTS[0], LAYOUTS[3]], ids=str)
