@@ -689,13 +689,24 @@ __device__ __forceinline__ void finish(const TreeAttn& P, const TreeItem& it, co
       l_tot = l_tot * f + __builtin_amdgcn_exp2f(sk - M);
     }
     const float inv = l_tot == 0.f ? 0.f : f / l_tot;
-    bf16* o = reinterpret_cast<bf16*>(P.o) + ((int64_t)(it.t0 + c.node[j]) * P.hq + c.head[j]) * D + 4 * h;
+    // the lanes of a column trade halves, so that each writes eight dims at a time
+    bf16* o = reinterpret_cast<bf16*>(P.o) + ((int64_t)(it.t0 + c.node[j]) * P.hq + c.head[j]) * D + 8 * h;
 #pragma unroll
     for (int dt = 0; dt < 2; ++dt)
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        store4(o + 32 * dt + 8 * q, make_float4(c.acc[dt][j][4 * q] * inv, c.acc[dt][j][4 * q + 1] * inv,
-                                                c.acc[dt][j][4 * q + 2] * inv, c.acc[dt][j][4 * q + 3] * inv));
+      for (int q = 0; q < 4; q += 2) {
+        uint32_t w[2][2];  // [q][pair of dims]
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const int e = 4 * (q + k) + 2 * r;
+            w[k][r] = pack_bf16(c.acc[dt][j][e] * inv, c.acc[dt][j][e + 1] * inv);
+          }
+        auto lo = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
+        auto hi = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+        *reinterpret_cast<u32x4_t*>(o + 32 * dt + 8 * q) = u32x4_t{lo[0], hi[0], lo[1], hi[1]};
+      }
   }
 }
 
