@@ -459,7 +459,7 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(TreeAttn P, int tiles) {
 // would pass 2^8, so that most steps have no cross-lane step and no rescale.
 //
 // Wide trees are bound by the vector pipe beside the products: 16 trees of 33-64 nodes
-// behind 8-16 K tokens take 196 us with the combine (640 TFLOP/s over the pairs in
+// behind 8-16 K tokens take 192 us with the combine (650 TFLOP/s over the pairs in
 // sight); without loads and barriers the same instructions take 85% of that. Narrow
 // trees are bound by HBM.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -1043,13 +1043,13 @@ __global__ __launch_bounds__(64, 3) void tree_attn_narrow_kernel(TreeAttn P, int
 // several column tiles they make each fetch its pages anew. Measured in us, 64 query
 // heads on 8 KV heads, six sets of pools in turn (contexts of 4-16 K tokens unless
 // given; NARROW2 was NARROW_STREAM with two column tiles a wavefront):
-//   up to 32 columns, 256 windowed trees of 1-4 nodes: NARROW_STREAM 20.3, NARROW 23.8; 48 trees of 1-4
+//   up to 32 columns, 256 windowed trees of 1-4 nodes: NARROW_STREAM 18.5, NARROW 21.8; 48 trees of 1-4
 //     NARROW_STREAM 102, NARROW 115, WIDE2 107; one tree of 4 behind 6 K NARROW 8.9, WIDE1 9.6
-//   few or one each, up to 96: 256 windowed trees of 2-12 NARROW 35, NARROW_STREAM 36, WIDE1 and WIDE2 39; one
+//   few or one each, up to 96: 256 windowed trees of 2-12 NARROW 32, NARROW_STREAM 32.5, WIDE2 34, WIDE1 36; one
 //     tree of 8 behind 6 K NARROW 9.8, WIDE1 10.5
-//   few or one each, above: 256 windowed trees of 8-16 WIDE1 45, WIDE2 47, NARROW 50; one tree of 16 behind 6 K
+//   few or one each, above: 256 windowed trees of 8-16 WIDE1 and WIDE2 41, NARROW 45; one tree of 16 behind 6 K
 //     WIDE1 11.8, NARROW 12.0, WIDE2 13.8, of 64 WIDE1 21.6, NARROW 22.2, WIDE4 23.2; 16 windowed trees of 17-30
-//     WIDE1 12.2, WIDE4 16.0
+//     NARROW 10.8, WIDE1 11.2, WIDE4 14.2
 //   up to 128, 48 trees of 1-8: WIDE2 113 + 5 for the combine, NARROW2 108 + 9, NARROW 162; 128 trees of 1-8 WIDE2
 //     311 + 9, NARROW2 303 + 13; 24 trees of 1-8 WIDE2 50 + 6, NARROW2 53 + 8; 48 trees of 8-16 WIDE2 121, WIDE1 128,
 //     WIDE4 162
