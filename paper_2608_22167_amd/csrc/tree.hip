@@ -6,8 +6,10 @@
 // tree read the same committed keys, so the matrix-core columns are (node, query
 // head) pairs of one KV head and a page is read once for all of them, where a
 // token-by-token step reads it once per token.
-//   plan     splits each tree's page range, and finds every node's ancestors
-//   attend   one split of one tree and KV head: running maximum, sum and values
+//   plan     splits each tree's page range (large split batches only: else each
+//            wavefront finds its split)
+//   attend   one split of one tree and KV head: the nodes' ancestors, running maximum,
+//            sum and values
 //   combine  merges the splits of trees that have several, with the sink
 #include <type_traits>
 
