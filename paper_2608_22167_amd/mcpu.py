@@ -164,6 +164,14 @@ def _buf(t, n, dtype=torch.int32) -> int:
     return t.data_ptr()
 
 
+def _ws(t) -> int:
+    """Address of a workspace."""
+    p = t.data_ptr()
+    if not t.is_cuda or p % 256 or not t.is_contiguous():
+        raise McpuError(MCPU_EINVAL, "a workspace lies on the GPU, 256-byte aligned")
+    return p
+
+
 _addressof, _view = ctypes.addressof, ctypes.c_char.from_buffer
 
 
@@ -346,7 +354,7 @@ def kv_pages_copy(pools, src, dst, host_src, host_dst, workspace, stream=None):
     if hs.size != n or hd.size != n or dst.shape[0] != n:
         raise McpuError(MCPU_EINVAL, "src, dst and their host copies differ in length")
     _check(lib().kv_pages_copy(_handles(pools), len(pools), n, _buf(src, n), _buf(dst, n), _host(hs), _host(hd),
-                               workspace.data_ptr(), workspace.nbytes, _stream_on(src, stream)))
+                               _ws(workspace), workspace.nbytes, _stream_on(src, stream)))
 
 
 def workspace(nbytes: int, device="cuda") -> torch.Tensor:
@@ -387,17 +395,18 @@ def tree_attention(shape, sinks, pool: KVPool, page_table, seq_lens, cu_q, paren
                    q, o, workspace, stream=None):
     hs, hc, batch, max_pages = _tree_batch(page_table, host_seq_lens, host_cu_q)
     n, width, dt = hc.item(batch), shape.n_q_heads * shape.head_dim, shape.torch_dtype
-    _check(lib().tree_attention(_cfg_for(shape, pool), _ptr(sinks), pool.handle, batch,
+    sk = None if sinks is None else _buf(sinks, shape.n_q_heads, torch.float32)
+    _check(lib().tree_attention(_cfg_for(shape, pool), sk, pool.handle, batch,
                                 _buf(page_table, batch * max_pages), max_pages, _buf(seq_lens, batch),
                                 _buf(cu_q, batch + 1), _buf(parents, n), _host(hs), _host(hc), _buf(q, n * width, dt),
-                                _buf(o, n * width, dt), workspace.data_ptr(), workspace.nbytes,
+                                _buf(o, n * width, dt), _ws(workspace), workspace.nbytes,
                                 _stream_on(q, stream)))
 
 
 def tree_accept(cu_q, parents, draft, sampled, path, n_path, next_tokens, workspace, stream=None):
     batch, n = cu_q.shape[0] - 1, parents.shape[0]
     _check(lib().tree_accept(batch, n, _buf(cu_q, 1), _buf(parents, n), _buf(draft, n), _buf(sampled, n),
-                             _buf(path, n), _buf(n_path, batch), _buf(next_tokens, batch), workspace.data_ptr(),
+                             _buf(path, n), _buf(n_path, batch), _buf(next_tokens, batch), _ws(workspace),
                              workspace.nbytes, _stream_on(parents, stream)))
 
 
@@ -406,7 +415,7 @@ def kv_tree_commit(pools, page_table, seq_lens, cu_q, path, n_path, workspace, s
     (batch, max_pages), n = page_table.shape, path.shape[0]
     _check(lib().kv_tree_commit(_handles(pools), len(pools), batch, _buf(page_table, batch * max_pages), max_pages,
                                 _buf(seq_lens, batch), _buf(cu_q, batch + 1), n, _buf(path, n), _buf(n_path, batch),
-                                workspace.data_ptr(), workspace.nbytes, _stream_on(path, stream)))
+                                _ws(workspace), workspace.nbytes, _stream_on(path, stream)))
 
 
 def moe_forward_workspace_size(shape, max_tokens) -> int:
@@ -456,8 +465,10 @@ def decode_layer_tree(shape, weights: DeviceWeights, pool: KVPool, page_table, s
                                    _buf(cu_q, batch + 1), _buf(parents, n), _host(hs), _host(hc),
                                    _buf(x_in, n * shape.hidden, torch.float32),
                                    _buf(x_out, n * shape.hidden, torch.float32),
-                                   _ptr(topk_idx), _ptr(topk_w), ctypes.byref(taps) if taps is not None else None,
-                                   workspace.data_ptr(), workspace.nbytes, _stream_on(x_in, stream)))
+                                   None if topk_idx is None else _buf(topk_idx, n * shape.top_k),
+                                   None if topk_w is None else _buf(topk_w, n * shape.top_k, torch.float32),
+                                   ctypes.byref(taps) if taps is not None else None, _ws(workspace),
+                                   workspace.nbytes, _stream_on(x_in, stream)))
 
 
 def decode_layer_noalloc(shape, weights: DeviceWeights, pool: KVPool, page_table, seq_lens, cu_q, host_seq_lens,

@@ -323,6 +323,12 @@ def test_refusals_of_tensors():
     for src, hs in ((two.cpu(), [0, 0]), (two.long(), [0, 0]), (two, [0])):
         with pytest.raises(mcpu.McpuError):
             mcpu.kv_pages_copy([pool], src, two, np.array(hs, np.int32), np.array([1, 2], np.int32), ws)
+    for bad in (ws.cpu(), ws[4:]):
+        with pytest.raises(mcpu.McpuError):
+            mcpu.tree_accept(good["cu"], good["par"], path, path, path.clone(), two, two.clone(), bad)
+    for bad in (c.sinks, c.sinks[:4].cuda(), c.sinks.cuda().double()):
+        with pytest.raises(mcpu.McpuError):
+            mcpu.tree_attention(s, bad, pool, *good.values(), ws)
     torch.cuda.synchronize()
     assert mcpu.mcpu_check_device_errors(ws) == 0
 
