@@ -267,6 +267,16 @@ class Generator:
             for lp, p in zip(missing, mcpu.kv_pages_alloc(self.alloc_sw, len(missing))):
                 s.pages_sw[lp] = int(p)
 
+    def _room(self, s: _Seq, q: int) -> bool:
+        """_grow, or False where there are too few pages (those taken stay with the sequence)."""
+        try:
+            self._grow(s, q)
+        except mcpu.McpuError as e:
+            if e.code != mcpu.MCPU_ENOMEM:
+                raise
+            return False
+        return True
+
     def _shrink(self, s: _Seq) -> None:
         """Free window pages wholly left of the next token's window."""
         lo = max(0, s.length - self.spec.window + 1) // PAGE
@@ -375,9 +385,10 @@ class Generator:
         are the tokens that calls of `step()` would have drawn. Sequences with
         longer input are left to `step()`; no more rows are fed than
         max_tokens_per_step, oldest sequences first and drafts only where every
-        sequence has its row."""
+        sequence has its row. A draft for which there are no rows or pages left, or
+        that passes the last position, is not tried."""
         ready = [s for s in self.seqs.values() if len(s.pending) == 1][:self.max_tokens]
-        batch, q_lens, toks, pars, depth, budget = [], [], [], [], [], self.max_tokens - len(ready)
+        trees, batch, q_lens, toks, pars, depth, budget = [], [], [], [], [], [], self.max_tokens - len(ready)
         for s in ready:
             d_tok, d_par = drafts.get(s.sid, ((), ()))
             if len(d_tok) != len(d_par) or len(d_tok) >= mcpu.TREE_MAX_NODES:
@@ -387,7 +398,11 @@ class Generator:
                 if not -1 <= p < i:
                     raise ValueError(f"draft of sequence {s.sid}: parent {p} of token {i}")
                 dep.append(dep[p + 1] + 1)
-            if len(d_tok) > budget:
+            trees.append((s, d_tok, d_par, dep))
+        for s in ready:
+            self._grow(s, 1)
+        for s, d_tok, d_par, dep in trees:
+            if len(d_tok) > budget or s.length + max(dep) >= self.spec.max_ctx or not self._room(s, 1 + len(d_tok)):
                 d_tok, d_par, dep = (), (), [0]
             budget -= len(d_tok)
             batch.append(s)
@@ -401,8 +416,6 @@ class Generator:
             self.tree_ws = mcpu.workspace(max(mcpu.decode_layer_tree_workspace_size(self.ss.shape(i), self.max_tokens,
                                                                                     self.max_tokens)
                                               for i in range(min(2, self.spec.n_layers))), self.device)
-        for s, q in zip(batch, q_lens):
-            self._grow(s, q)
         x, cu, d = self._forward(batch, q_lens, np.array(toks, np.int64), np.array(pars, np.int32))
         dev, T, B = self.device, len(toks), len(batch)
         up = lambda a: torch.from_numpy(np.array(a, np.int32)).to(dev)  # noqa: E731

@@ -294,6 +294,34 @@ def test_generator_group_shares_its_prompt(length):
     assert gen.free_pages() == free0
 
 
+def test_generator_drafts_that_do_not_fit_are_not_tried():
+    """Too few pages, or positions past the last one: such a step draws one token, the one that step() draws."""
+    spec = _spec(seed=3009, pages_full=9, pages_sw=9, max_ctx=128)
+    gen = Generator(spec, max_tokens_per_step=256)
+    prompt = np.random.default_rng(71).integers(0, spec.vocab, 100).tolist()
+    drawn = []
+    for tree in (False, True):
+        gen.add(0, prompt)
+        out = [t for t, _ in [gen.step()[0]]]
+        while len(out) < 29:  # token k of them sits at position 99 + k; the last one fed is number 28, at 127
+            if tree:
+                # 60 siblings need a tenth page; a chain of 20 behind token 9 or later passes position 127
+                n, chain = (60, False) if len(out) < 9 else (20, True)
+                known = (drawn[0][len(out):] + [1] * n)[:n]
+                got = gen.step_tree({0: (known, list(range(-1, n - 1)) if chain else [-1] * n)})[0]
+                assert len(got) == 1
+                out += [t for t, _ in got]
+            else:
+                out.append(gen.step()[0][0])
+        assert gen.check_errors() == 0
+        drawn.append(out)
+        with pytest.raises(mcpu.McpuError):  # position 128
+            gen.step_tree({}) if tree else gen.step()
+        gen.release(0)
+    assert drawn[0] == drawn[1]
+    assert gen.free_pages() == (9, 9)
+
+
 def test_generator_fork_in_mid_trajectory_and_when_pages_run_out():
     spec = _spec(seed=3008, pages_full=24, pages_sw=24)
     gen = Generator(spec, max_tokens_per_step=256)
