@@ -268,14 +268,25 @@ class Generator:
                 s.pages_sw[lp] = int(p)
 
     def _room(self, s: _Seq, q: int) -> bool:
-        """_grow, or False where there are too few pages (those taken stay with the sequence)."""
+        """_grow, or False where there are too few pages (only the pending token's stay with the sequence)."""
         try:
             self._grow(s, q)
         except mcpu.McpuError as e:
             if e.code != mcpu.MCPU_ENOMEM:
                 raise
+            self._trim(s, s.length + 1)
             return False
         return True
+
+    def _trim(self, s: _Seq, n: int) -> None:
+        """Free the pages behind position n - 1, which drafted tokens that did not stay have taken."""
+        keep = (n + PAGE - 1) // PAGE
+        if len(s.pages_full) > keep:
+            mcpu.kv_pages_free(self.alloc_full, np.array(s.pages_full[keep:], np.int32))
+            del s.pages_full[keep:]
+        behind = [lp for lp in s.pages_sw if lp >= keep]
+        if behind:
+            mcpu.kv_pages_free(self.alloc_sw, np.array([s.pages_sw.pop(lp) for lp in behind], np.int32))
 
     def _shrink(self, s: _Seq) -> None:
         """Free window pages wholly left of the next token's window."""
@@ -291,7 +302,7 @@ class Generator:
         pt_f = -np.ones((len(batch), max_lp), np.int32)
         pt_s = -np.ones((len(batch), max_lp), np.int32)
         for b, s in enumerate(batch):
-            own = s.pages_full[:max_lp]  # a tree step may have left pages behind the last position
+            own = s.pages_full[:max_lp]  # a step that failed may have left pages behind the last position
             pt_f[b, :len(own)] = own
             for lp, p in s.pages_sw.items():
                 if lp < max_lp:
@@ -386,10 +397,11 @@ class Generator:
         longer input are left to `step()`; no more rows are fed than
         max_tokens_per_step, oldest sequences first and drafts only where every
         sequence has its row. A draft for which there are no rows or pages left, or
-        that passes the last position, is not tried."""
-        ready = [s for s in self.seqs.values() if len(s.pending) == 1][:self.max_tokens]
-        trees, batch, q_lens, toks, pars, depth, budget = [], [], [], [], [], [], self.max_tokens - len(ready)
-        for s in ready:
+        that passes the last position, is not tried. Pages of tokens that did not
+        stay are free again when the call returns or fails, so that a sequence
+        holds what `step()` would have left it with."""
+        trees = []
+        for s in [s for s in self.seqs.values() if len(s.pending) == 1][:self.max_tokens]:
             d_tok, d_par = drafts.get(s.sid, ((), ()))
             if len(d_tok) != len(d_par) or len(d_tok) >= mcpu.TREE_MAX_NODES:
                 raise ValueError(f"draft of sequence {s.sid}: {len(d_tok)} tokens, {len(d_par)} parents")
@@ -399,7 +411,16 @@ class Generator:
                     raise ValueError(f"draft of sequence {s.sid}: parent {p} of token {i}")
                 dep.append(dep[p + 1] + 1)
             trees.append((s, d_tok, d_par, dep))
-        for s in ready:
+        try:
+            return self._step_trees(trees)
+        finally:
+            for s, *_ in trees:
+                self._trim(s, s.length)
+
+    def _step_trees(self, trees) -> Dict[int, List[tuple]]:
+        """step_tree of checked drafts: (sequence, tokens, parents, depths from the pending token on)."""
+        batch, q_lens, toks, pars, depth, budget = [], [], [], [], [], self.max_tokens - len(trees)
+        for s, *_ in trees:
             self._grow(s, 1)
         for s, d_tok, d_par, dep in trees:
             if len(d_tok) > budget or s.length + max(dep) >= self.spec.max_ctx or not self._room(s, 1 + len(d_tok)):
