@@ -184,8 +184,8 @@ class Generator:
     def fork(self, sid: int, new_sids: Sequence[int]) -> None:
         """Start each of new_sids as a copy of sequence sid (cache, history and
         pending input): whole pages get another holder, a partly filled last
-        page is copied for each. All or nothing: MCPU_ENOMEM leaves every
-        sequence as it was."""
+        page is copied for each. All or nothing: a fork that fails (MCPU_ENOMEM:
+        too few pages) leaves every sequence and page as it was."""
         s, n = self.seqs[sid], len(new_sids)
         if len(set(new_sids)) != n or any(k in self.seqs for k in new_sids):
             raise ValueError(f"fork: sequence ids {list(new_sids)} repeat or exist")
@@ -200,20 +200,25 @@ class Generator:
             if alloc is not None:
                 kinds.append((alloc, pools, shared, last if part else []))
         copies: List[np.ndarray] = []
+        taken: List[tuple] = []  # (allocator, pages), a holder each
         try:
-            for alloc, _, _, last in kinds:
+            for alloc, _, shared, last in kinds:
                 copies.append(mcpu.kv_pages_alloc(alloc, n * len(last)))
-        except mcpu.McpuError:
-            for (alloc, _, _, _), ids in zip(kinds, copies):
-                mcpu.kv_pages_free(alloc, ids)
-            raise
-        for (alloc, pools, shared, last), ids in zip(kinds, copies):
-            mcpu.kv_pages_share(alloc, np.array(shared * n, np.int32))
-            if last:
+                taken.append((alloc, copies[-1]))
+                for _ in range(n):
+                    mcpu.kv_pages_share(alloc, shared)
+                    taken.append((alloc, shared))
+            for (_, pools, _, last), ids in zip(kinds, copies):
+                if not last:
+                    continue
                 src = np.full(n, last[0], np.int32)
                 d_src, d_dst = (torch.from_numpy(np.ascontiguousarray(a, np.int32)).to(self.device) for a in (src, ids))
                 for i in range(0, len(pools), mcpu.MAX_POOLS):
                     mcpu.kv_pages_copy(pools[i:i + mcpu.MAX_POOLS], d_src, d_dst, src, ids, self.ws)
+        except BaseException:
+            for alloc, ids in taken:
+                mcpu.kv_pages_free(alloc, ids)
+            raise
         full = copies[0] if self.alloc_full is not None else np.zeros(0, np.int32)
         for j, k in enumerate(new_sids):
             c = _Seq(k, s.length, list(s.pending), s.pages_full[:whole], {}, list(s.history))
@@ -246,7 +251,7 @@ class Generator:
                 s.length += q
                 self._shrink(s)
             self.fork(sids[0], sids[1:])
-        except mcpu.McpuError:
+        except BaseException:
             self.release(sids[0])
             raise
 

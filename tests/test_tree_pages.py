@@ -151,3 +151,42 @@ def test_a_step_that_fails_gives_its_draft_pages_back():
         gen.step_tree({0: wrong(50)})
     assert (state(gen), gen.free_pages()) == before
     assert gen.step_tree({0: ([token(0, 11)], [-1])})[0] == [(token(0, 11), 0.0), (token(0, 12), 0.0)]
+
+
+@pytest.mark.parametrize("error", [mcpu.McpuError(mcpu.MCPU_EHIP, "a launch failed"), RuntimeError("out of memory")])
+@pytest.mark.parametrize("fail_at", [1, 2])
+def test_a_fork_that_fails_leaves_every_page_as_it_was(monkeypatch, error, fail_at):
+    """The copy of the last page fails for the first or the second kind: no page is shared, taken or forgotten."""
+    gen = Stub(32, 32)
+    gen.add(0, range(40))
+    gen.step()
+    holders = lambda: [mcpu.kv_page_holders(p, i) for p in gen.pools for i in range(32)]  # noqa: E731
+    before = state(gen), gen.free_pages(), holders()
+    calls = []
+
+    def copy(*a):
+        calls.append(a)
+        if len(calls) == fail_at:
+            raise error
+
+    monkeypatch.setattr(mcpu, "kv_pages_copy", copy)
+    with pytest.raises(type(error)):
+        gen.fork(0, [1, 2, 3])
+    assert len(calls) == fail_at and (state(gen), gen.free_pages(), holders()) == before
+    gen.fork(0, [1, 2, 3])
+    assert state(gen) == {sid: (40, 3, [0, 1, 2]) for sid in range(4)}
+    for sid in range(4):
+        gen.release(sid)
+    assert gen.free_pages() == (32, 32)
+
+
+def test_a_group_that_fails_leaves_no_sequence(monkeypatch):
+    gen = Stub(32, 32)
+
+    def copy(*a):
+        raise RuntimeError("out of memory")
+
+    monkeypatch.setattr(mcpu, "kv_pages_copy", copy)
+    with pytest.raises(RuntimeError):
+        gen.add_group([4, 5], range(40))
+    assert not gen.seqs and gen.free_pages() == (32, 32)
