@@ -236,6 +236,12 @@ __device__ __forceinline__ void write_rows(const TreeAttn& P, const TreeItem& it
     P.tok[it.t0 + lane] = make_int4(it.row0 + lane, it.n, it.splits, 0);
 }
 
+// A sink's share of the normaliser over the maximum M (log2 units). A sink of -inf has
+// none, also where there is no key (M = -inf).
+__device__ __forceinline__ float sink_term(float sink, float M) {
+  return M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sink - M);
+}
+
 // ---------------------------------------------------------------------------
 // attend, any type and head dim: 16 columns per wavefront
 // ---------------------------------------------------------------------------
@@ -436,7 +442,7 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(TreeAttn P, int tiles) {
   if (P.sinks) {
     const float sk = P.sinks[head] * LOG2E, M = fmaxf(m, sk);
     f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
-    l = l * f + __builtin_amdgcn_exp2f(sk - M);
+    l = l * f + sink_term(sk, M);
   }
   T* o = reinterpret_cast<T*>(P.o) + ((int64_t)(it.t0 + node) * P.hq + head) * D + 4 * grp;
 #pragma unroll
@@ -688,7 +694,7 @@ __device__ __forceinline__ void finish(const TreeAttn& P, const TreeItem& it, co
     if (P.sinks) {
       const float sk = P.sinks[c.head[j]] * LOG2E, M = fmaxf(c.m_run[j], sk);
       f = c.m_run[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(c.m_run[j] - M);
-      l_tot = l_tot * f + __builtin_amdgcn_exp2f(sk - M);
+      l_tot = l_tot * f + sink_term(sk, M);
     }
     const float inv = l_tot == 0.f ? 0.f : f / l_tot;
     // the lanes of a column trade halves, so that each writes eight dims at a time
@@ -1168,7 +1174,7 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeCombine P) {
       a.z += __shfl_xor(a.z, o, 64);
       a.w += __shfl_xor(a.w, o, 64);
     }
-  if (P.sinks) L += __builtin_amdgcn_exp2f(sink - Mt);
+  if (P.sinks) L += sink_term(sink, Mt);
   if (MANY && sub != 0) return;
   const float inv = L == 0.f ? 0.f : 1.0f / L;
   store4(reinterpret_cast<T*>(P.o) + ((int64_t)t * P.hq + h) * D + dim,
