@@ -76,7 +76,8 @@ enum {
   MCPU_DEVERR_ROPE = 2,  /* a position was >= rope_max_pos; that token's q/k were not written */
   MCPU_DEVERR_EXPERT = 4, /* a top-k expert id outside [0, n_experts) was passed in */
   MCPU_DEVERR_PLAN = 8,   /* device seq_lens / cu_q (or n_path) disagree with the host copies or their own
-                             limits; of a tree's calls, such a tree is left out */
+                             limits; of a tree's calls, a tree that has no place in the host's plan is
+                             left out (see tree_attention) */
   MCPU_DEVERR_MXFP4 = 16, /* an MXFP4 block scale outside [2, 252]: scaled values would not be
                              normal bfloat16; that block contributed zero */
   MCPU_DEVERR_TOKEN = 32, /* a token id outside [0, vocab) (embed_tokens); its row was zeroed */
@@ -312,7 +313,10 @@ enum { MCPU_TREE_MAX_NODES = 64 };
  * hold.
  *  cu_q (device) and host_cu_q are required, as are host_seq_lens; parents:
  *  device int32 [n_tokens]. Each tree has up to MCPU_TREE_MAX_NODES nodes, else
- *  MCPU_EUNSUPPORTED. Rows of q and o outside the trees do not exist. */
+ *  MCPU_EUNSUPPORTED. Rows of q and o outside the trees do not exist.
+ *  A tree that has no place in the plan made from the host's copies, because the
+ *  device's arrays differ (a negative or longer length, other rows), sets
+ *  MCPU_DEVERR_PLAN, and its rows of o stay as they were. */
 size_t tree_attention_workspace_size(const mcpu_layer_cfg* cfg, int32_t max_batch, int32_t max_tokens);
 int tree_attention(const mcpu_layer_cfg* cfg, const float* sinks, mcpu_kv_pool* pool, int32_t batch,
                    const int32_t* page_table, int32_t max_pages, const int32_t* seq_lens, const int32_t* cu_q,
@@ -399,7 +403,8 @@ int decode_layer(const mcpu_layer_cfg* cfg, const mcpu_layer_weights* w, mcpu_kv
  * positions p_i and tree_attention over the pages. Cache positions seq_lens[b] ..
  * seq_lens[b] + n - 1 receive the nodes' K and V; kv_tree_commit keeps the accepted
  * ones. cu_q, host_cu_q and parents (device int32 [n_tokens]) are required; a node
- * whose position lies beyond the RoPE table sets MCPU_DEVERR_ROPE. */
+ * whose position lies beyond the RoPE table sets MCPU_DEVERR_ROPE, and the rows of a
+ * tree that tree_attention leaves out are undefined in x_out. */
 size_t decode_layer_tree_workspace_size(const mcpu_layer_cfg* cfg, int32_t max_batch, int32_t max_tokens);
 int decode_layer_tree(const mcpu_layer_cfg* cfg, const mcpu_layer_weights* w, mcpu_kv_pool* pool, int32_t batch,
                       const int32_t* page_table, int32_t max_pages, const int32_t* seq_lens, const int32_t* cu_q,

@@ -8,8 +8,8 @@ namespace mcpu {
 
 constexpr int TREE_MAX_NODES = 64;  // a node's ancestors are the bits of one 64-bit word
 
-// One split of a tree's visible pages: n nodes (rows t0 ..) of sequence b behind
-// len committed tokens, logical pages pg0 .. pg1 - 1. Its partial rows (node i of
+// One split of a tree's visible pages: n nodes (rows t0 ..) of sequence b (-1: no
+// split) behind len committed tokens, logical pages pg0 .. pg1 - 1. Its partial rows (node i of
 // part_ml / part_acc at row0 + i) exist where the tree has more than one split; a
 // tree's only split writes o itself.
 struct TreeItem {
@@ -27,6 +27,7 @@ struct TreeArgs {
   int n_items, n_rows;      // splits and partial rows as the host counted them, checked on the device; without
                             // partial rows item i is tree i (n_items = batch)
   const TreeItem* item;     // [n_items] from the plan kernel, or nullptr
+  int4* tok;                // [n_tokens] where n_rows > 0: first partial row, rows per split, splits (0: no such tree)
   int32_t* err;
 };
 hipError_t launch_tree_plan(const TreeArgs& p, TreeItem* out, hipStream_t s);
@@ -51,7 +52,6 @@ struct TreeAttn : TreeArgs {
   const float* sinks;  // [Hq] or nullptr
   float* part_ml;      // [n_rows][Hq][2] running max (log2 units) and sum
   float* part_acc;     // [n_rows][Hq][D]
-  int4* tok;           // [n_tokens] out where n_rows > 0: first partial row, rows per split, splits
   void* o;             // [n_tokens][Hq * D]
 };
 hipError_t launch_tree_attn(int dtype, int head_dim, const TreeAttn& p, hipStream_t s);

@@ -569,6 +569,7 @@ int run_tree_attention(const mcpu_layer_cfg* c, const float* sinks, mcpu_kv_pool
                        int32_t* err, hipStream_t st) {
   TreeAttn ta{};
   static_cast<TreeArgs&>(ta) = tree_args(c, batch, max_pages, seq_lens, cu_q, parents, ph, err);
+  ta.tok = tb.tok;
   if (batch > TREE_SCAN && ph.n_rows > 0) {
     Timed tm(MCPU_KERNEL_TREE_PLAN, st);
     HIP_TRY(launch_tree_plan(ta, tb.item, st));
@@ -578,7 +579,7 @@ int run_tree_attention(const mcpu_layer_cfg* c, const float* sinks, mcpu_kv_pool
   ta.form = ph.form;
   ta.hq = c->n_q_heads; ta.hkv = c->n_kv_heads;
   ta.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c->head_dim));
-  ta.sinks = sinks; ta.part_ml = tb.part_ml; ta.part_acc = tb.part_acc; ta.tok = tb.tok; ta.o = o;
+  ta.sinks = sinks; ta.part_ml = tb.part_ml; ta.part_acc = tb.part_acc; ta.o = o;
   {
     Timed tm(MCPU_KERNEL_TREE_ATTN, st);
     HIP_TRY(launch_tree_attn(c->dtype, c->head_dim, ta, st));

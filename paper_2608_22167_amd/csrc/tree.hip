@@ -61,18 +61,30 @@ __device__ __forceinline__ TreeItem split_of(const TreeArgs& P, const TreeSpan& 
   return it;
 }
 
+// Has a tree whose first split is item `at`, and whose first partial row is row0, a
+// place in the host's plan? One that has not (device arrays that disagree with the
+// host's) is left out as a whole.
+__device__ __forceinline__ bool placed(const TreeArgs& P, const TreeSpan& s, int at, int row0) {
+  return s.n > 0 && at >= 0 && at <= P.n_items - s.splits && row0 >= 0 && row0 <= P.n_rows - rows_of(s);
+}
+
 // The plan of a large batch, by one workgroup: a thread per sequence, and the
-// records of a wavefront's 64 trees written together, lane j the j-th.
+// records of a wavefront's 64 trees written together, lane j the j-th. Where the
+// device's arrays disagree with the host's plan, the records that no tree has and all
+// rows are marked as such, since an earlier call may have left others there.
 __global__ __launch_bounds__(1024) void tree_plan_kernel(TreeArgs P, TreeItem* out) {
   __shared__ int sums[2][16];
+  __shared__ int bad;
   const int lane = lane_id(), wave = threadIdx.x >> 6;
+  const bool covered = P.cu_q[0] == 0 && P.cu_q[P.batch] == P.n_tokens;
+  if (threadIdx.x == 0) bad = !covered;
   int items = 0, rows = 0;
   for (int base = 0; base < P.batch; base += 1024) {
     const int b = base + threadIdx.x;
     const TreeSpan s = tree_span(P, b);
-    if (s.bad) set_error(P.err, 8);
     const int incl = wave_incl_scan(s.splits), rincl = wave_incl_scan(rows_of(s));
     __syncthreads();  // sums may still be read for the tile before
+    if (s.bad) bad = 1;
     if (lane == 63) {
       sums[0][wave] = incl;
       sums[1][wave] = rincl;
@@ -85,6 +97,7 @@ __global__ __launch_bounds__(1024) void tree_plan_kernel(TreeArgs P, TreeItem* o
       items += sums[0][w];
       rows += sums[1][w];
     }
+    const int in = placed(P, s, at + incl - s.splits, row0);
     const int all = __shfl(incl, 63, 64);
     for (int j0 = 0; j0 < all; j0 += 64) {
       const int j = j0 + lane;
@@ -96,10 +109,15 @@ __global__ __launch_bounds__(1024) void tree_plan_kernel(TreeArgs P, TreeItem* o
       r.t0 = __shfl(s.t0, src, 64); r.n = __shfl(s.n, src, 64); r.len = __shfl(s.len, src, 64);
       r.pages = __shfl(s.pages, src, 64); r.splits = __shfl(s.splits, src, 64);
       const int k = j - (__shfl(incl, src, 64) - r.splits), rb = __shfl(b, src, 64), rr = __shfl(row0, src, 64);
-      if (j < all && at + j < P.n_items) out[at + j] = split_of(P, r, rb, rr, k);
+      const int rin = __shfl(in, src, 64);
+      if (j < all && at + j >= 0 && at + j < P.n_items) out[at + j] = split_of(P, r, rin ? rb : -1, rr, k);
     }
   }
-  if (threadIdx.x == 0 && (items != P.n_items || rows != P.n_rows)) set_error(P.err, 8);
+  __syncthreads();
+  if (!bad && items == P.n_items && rows == P.n_rows) return;
+  if (threadIdx.x == 0) set_error(P.err, 8);
+  for (int i = max(0, items) + threadIdx.x; i < P.n_items; i += 1024) out[i].b = -1;
+  for (int t = threadIdx.x; t < P.n_tokens; t += 1024) P.tok[t] = make_int4(0, 0, 0, 0);
 }
 
 hipError_t launch_tree_plan(const TreeArgs& p, TreeItem* out, hipStream_t s) {
@@ -112,8 +130,7 @@ hipError_t launch_tree_plan(const TreeArgs& p, TreeItem* out, hipStream_t s) {
 // split, item i is tree i. Otherwise, up to TREE_SCAN sequences, each wavefront
 // finds it by itself, four sequences per lane: one round of memory instead of a
 // launch in front of the step (48 trees 7 us, one tree 5 us). Larger batches read
-// the plan kernel's records, every field checked before it addresses memory, since
-// one that the plan did not write may be stale.
+// the plan kernel's records, every field checked before it addresses memory.
 __device__ __forceinline__ bool find_item(const TreeArgs& P, int i, TreeItem& it) {
   bool ok = false;
   it = TreeItem{};
@@ -133,14 +150,15 @@ __device__ __forceinline__ bool find_item(const TreeArgs& P, int i, TreeItem& it
     TreeSpan s[TREE_SCAN / 64];
 #pragma unroll
     for (int c = 0; c < TREE_SCAN / 64; ++c) s[c] = tree_span(P, 64 * c + lane);
-    int items = 0, rows = 0;
+    int items = 0, rows = 0, end = 0;
     bool bad = false;
 #pragma unroll
     for (int c = 0; c < TREE_SCAN / 64; ++c) {
       if (64 * c >= P.batch) break;
       const int incl = wave_incl_scan(s[c].splits), rincl = wave_incl_scan(rows_of(s[c]));
+      const bool in = placed(P, s[c], items + incl - s[c].splits, rows + rincl - rows_of(s[c]));
       const uint64_t past = __ballot(items + incl > i);
-      if (!ok && past != 0) {  // uniform
+      if (it.n == 0 && past != 0) {  // uniform
         const int src = (int)__builtin_ctzll(past);
         TreeSpan r;
         r.t0 = __builtin_amdgcn_readlane(s[c].t0, src); r.n = __builtin_amdgcn_readlane(s[c].n, src);
@@ -148,13 +166,27 @@ __device__ __forceinline__ bool find_item(const TreeArgs& P, int i, TreeItem& it
         r.splits = __builtin_amdgcn_readlane(s[c].splits, src);
         const int k = i - (items + __builtin_amdgcn_readlane(incl, src) - r.splits);
         it = split_of(P, r, 64 * c + src, rows + __builtin_amdgcn_readlane(rincl, src) - rows_of(r), k);
-        ok = it.splits == 1 || it.row0 <= P.n_rows - it.n;
+        ok = __builtin_amdgcn_readlane(in, src);
       }
       items += __builtin_amdgcn_readlane(incl, 63);
       rows += __builtin_amdgcn_readlane(rincl, 63);
+      end = __builtin_amdgcn_readlane(s[c].t0 + s[c].n, min(P.batch - 1 - 64 * c, 63));
       bad |= s[c].bad;
+      s[c].n = in ? s[c].n : 0;
     }
-    if (i == 0 && (bad || items != P.n_items || rows != P.n_rows)) set_error(P.err, 8);
+    const bool covered = __builtin_amdgcn_readlane(s[0].t0, 0) == 0 && end == P.n_tokens;
+    if (i == 0 && (__ballot(bad) != 0 || !covered || items != P.n_items || rows != P.n_rows)) {
+      // rare: the rows of no tree are marked as such, as an earlier call may have left records there
+      if (lane == 0) set_error(P.err, 8);
+      for (int t = lane; t < P.n_tokens + lane; t += 64) {
+        bool mine = false;
+#pragma unroll
+        for (int c = 0; c < TREE_SCAN / 64; ++c)
+          for (int src = 0; src < 64; ++src)
+            mine |= (uint32_t)(t - __builtin_amdgcn_readlane(s[c].t0, src)) < (uint32_t)__builtin_amdgcn_readlane(s[c].n, src);
+        if (!mine && t < P.n_tokens) P.tok[t] = make_int4(0, 0, 0, 0);
+      }
+    }
   }
   it.b = uniform(it.b); it.t0 = uniform(it.t0); it.n = uniform(it.n); it.len = uniform(it.len);
   it.pg0 = uniform(it.pg0); it.pg1 = uniform(it.pg1); it.row0 = uniform(it.row0); it.splits = uniform(it.splits);
@@ -1117,7 +1149,7 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeCombine P) {
   if (t >= P.n_tokens) return;
   const int4 tok = P.tok[t];
   const int row0 = tok.x, n = tok.y, splits = MANY ? uniform(tok.z) : tok.z;
-  // a stale record (device arrays that disagree with the plan) stays inside the partial rows
+  // rows without splits, and rows of no tree
   if (splits <= 1 || row0 < 0 || n <= 0 || n > TREE_MAX_NODES || (int64_t)row0 + (int64_t)(splits - 1) * n >= P.n_rows) return;
   const float sink = P.sinks ? P.sinks[h] * LOG2E : 0.f;
   float M = -INFINITY, L = 0.f;
