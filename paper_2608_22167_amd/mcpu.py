@@ -156,20 +156,35 @@ def _stream(stream=None):
 # is kept short: pointers and the raw stream without objects in between.
 
 
-def _buf(t, n, dtype=torch.int32) -> int:
-    """Address of a contiguous device tensor of at least n elements of a type."""
-    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous() or not t.is_cuda:
-        raise McpuError(MCPU_EINVAL, f"a contiguous {dtype} tensor of {n} elements or more on the GPU is needed, "
+def _device(t) -> int:
+    """The device of a call, which is its first tensor's and has to be the current one."""
+    dev = t.get_device()  # of a tensor on a GPU, so that torch has set up its devices
+    if dev < 0 or dev != torch._C._cuda_getDevice():
+        raise McpuError(MCPU_EINVAL, f"a tensor on the current GPU is needed, got one on {t.device}")
+    return dev
+
+
+def _buf(t, n, dev, dtype=torch.int32) -> int:
+    """Address of a contiguous tensor of at least n elements of a type on the call's device."""
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous() or t.get_device() != dev:
+        raise McpuError(MCPU_EINVAL, f"a contiguous {dtype} tensor of {n} elements or more on GPU {dev} is needed, "
                                      f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
     return t.data_ptr()
 
 
-def _ws(t) -> int:
+def _ws(t, dev) -> int:
     """Address of a workspace."""
     p = t.data_ptr()
-    if not t.is_cuda or p % 256 or not t.is_contiguous():
-        raise McpuError(MCPU_EINVAL, "a workspace lies on the GPU, 256-byte aligned")
+    if t.get_device() != dev or p % 256 or not t.is_contiguous():
+        raise McpuError(MCPU_EINVAL, f"a workspace lies on the call's GPU {dev}, 256-byte aligned")
     return p
+
+
+def _pool(pool, dev):
+    """The handle of a pool on the call's device."""
+    if pool.device != dev:
+        raise McpuError(MCPU_EINVAL, f"the pool's K and V lie on {pool.k.device} and {pool.v.device}, the call's GPU is {dev}")
+    return pool.handle
 
 
 _addressof, _view = ctypes.addressof, ctypes.c_char.from_buffer
@@ -180,12 +195,13 @@ def _host(a: np.ndarray) -> int:
     return _addressof(_view(a)) if a.size and a.flags.writeable else a.ctypes.data
 
 
-def _stream_on(t, stream=None) -> int:
-    """The stream to launch on: `stream`, or the current one; the tensors have to live on the current device."""
-    dev = t.get_device()  # of a tensor on the GPU, so that torch has set up its devices
-    if dev < 0 or dev != torch._C._cuda_getDevice():
-        raise McpuError(MCPU_EINVAL, f"tensors on device {dev}, current device {torch.cuda.current_device()}")
-    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(dev)
+def _stream_on(dev, stream=None) -> int:
+    """The stream to launch on: `stream`, or the current one."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        raise McpuError(MCPU_EINVAL, f"a stream of GPU {stream.device_index}, the call's is {dev}")
+    return stream.cuda_stream
 
 
 def _cfg_for(shape, pool):
@@ -287,6 +303,7 @@ class KVPool:
         self.cfg = make_cfg(shape)
         self.k, self.v = k_pool, v_pool
         self.n_pages = int(k_pool.shape[0])
+        self.device = k_pool.get_device() if k_pool.get_device() == v_pool.get_device() else -1
         h = ctypes.c_void_p()
         _check(lib().kv_pool_create(ctypes.byref(self.cfg), self.n_pages, _ptr(k_pool), _ptr(v_pool),
                                     ctypes.byref(h)))
@@ -344,8 +361,8 @@ def kv_page_holders(pool: KVPool, page: int) -> int:
     return n
 
 
-def _handles(pools):
-    return (ctypes.c_void_p * len(pools))(*[p.handle for p in pools])
+def _handles(pools, dev):
+    return (ctypes.c_void_p * len(pools))(*[p.handle if p.device == dev else _pool(p, dev) for p in pools])
 
 
 def kv_pages_copy(pools, src, dst, host_src, host_dst, workspace, stream=None):
@@ -353,8 +370,9 @@ def kv_pages_copy(pools, src, dst, host_src, host_dst, workspace, stream=None):
     hs, hd, n = _host_i32(host_src), _host_i32(host_dst), src.shape[0]
     if hs.size != n or hd.size != n or dst.shape[0] != n:
         raise McpuError(MCPU_EINVAL, "src, dst and their host copies differ in length")
-    _check(lib().kv_pages_copy(_handles(pools), len(pools), n, _buf(src, n), _buf(dst, n), _host(hs), _host(hd),
-                               _ws(workspace), workspace.nbytes, _stream_on(src, stream)))
+    dev = _device(src)
+    _check(lib().kv_pages_copy(_handles(pools, dev), len(pools), n, _buf(src, n, dev), _buf(dst, n, dev), _host(hs),
+                               _host(hd), _ws(workspace, dev), workspace.nbytes, _stream_on(dev, stream)))
 
 
 def workspace(nbytes: int, device="cuda") -> torch.Tensor:
@@ -386,6 +404,8 @@ def _tree_batch(page_table, host_seq_lens, host_cu_q):
     """Host lengths and row offsets, and the batch and width of the page table they have to fit."""
     hs, hc = _host_i32(host_seq_lens), _host_i32(host_cu_q)
     batch, max_pages = page_table.shape
+    if hs is None or hc is None:
+        raise McpuError(MCPU_EINVAL, "host_seq_lens and host_cu_q are needed")
     if hs.size != batch or hc.size != batch + 1:
         raise McpuError(MCPU_EINVAL, f"host copies of {hs.size} lengths and {hc.size} row offsets for {batch} sequences")
     return hs, hc, batch, max_pages
@@ -394,28 +414,30 @@ def _tree_batch(page_table, host_seq_lens, host_cu_q):
 def tree_attention(shape, sinks, pool: KVPool, page_table, seq_lens, cu_q, parents, host_seq_lens, host_cu_q,
                    q, o, workspace, stream=None):
     hs, hc, batch, max_pages = _tree_batch(page_table, host_seq_lens, host_cu_q)
-    n, width, dt = hc.item(batch), shape.n_q_heads * shape.head_dim, shape.torch_dtype
-    sk = None if sinks is None else _buf(sinks, shape.n_q_heads, torch.float32)
-    _check(lib().tree_attention(_cfg_for(shape, pool), sk, pool.handle, batch,
-                                _buf(page_table, batch * max_pages), max_pages, _buf(seq_lens, batch),
-                                _buf(cu_q, batch + 1), _buf(parents, n), _host(hs), _host(hc), _buf(q, n * width, dt),
-                                _buf(o, n * width, dt), _ws(workspace), workspace.nbytes,
-                                _stream_on(q, stream)))
+    n, width, dt, dev = hc.item(batch), shape.n_q_heads * shape.head_dim, shape.torch_dtype, _device(q)
+    sk = None if sinks is None else _buf(sinks, shape.n_q_heads, dev, torch.float32)
+    _check(lib().tree_attention(_cfg_for(shape, pool), sk, _pool(pool, dev), batch,
+                                _buf(page_table, batch * max_pages, dev), max_pages, _buf(seq_lens, batch, dev),
+                                _buf(cu_q, batch + 1, dev), _buf(parents, n, dev), _host(hs), _host(hc),
+                                _buf(q, n * width, dev, dt), _buf(o, n * width, dev, dt), _ws(workspace, dev),
+                                workspace.nbytes, _stream_on(dev, stream)))
 
 
 def tree_accept(cu_q, parents, draft, sampled, path, n_path, next_tokens, workspace, stream=None):
-    batch, n = cu_q.shape[0] - 1, parents.shape[0]
-    _check(lib().tree_accept(batch, n, _buf(cu_q, 1), _buf(parents, n), _buf(draft, n), _buf(sampled, n),
-                             _buf(path, n), _buf(n_path, batch), _buf(next_tokens, batch), _ws(workspace),
-                             workspace.nbytes, _stream_on(parents, stream)))
+    batch, n, dev = cu_q.shape[0] - 1, parents.shape[0], _device(cu_q)
+    _check(lib().tree_accept(batch, n, _buf(cu_q, 1, dev), _buf(parents, n, dev), _buf(draft, n, dev),
+                             _buf(sampled, n, dev), _buf(path, n, dev), _buf(n_path, batch, dev),
+                             _buf(next_tokens, batch, dev), _ws(workspace, dev), workspace.nbytes,
+                             _stream_on(dev, stream)))
 
 
 def kv_tree_commit(pools, page_table, seq_lens, cu_q, path, n_path, workspace, stream=None):
     """Keep an accepted path in every pool of `pools` (the layers that page_table belongs to)."""
-    (batch, max_pages), n = page_table.shape, path.shape[0]
-    _check(lib().kv_tree_commit(_handles(pools), len(pools), batch, _buf(page_table, batch * max_pages), max_pages,
-                                _buf(seq_lens, batch), _buf(cu_q, batch + 1), n, _buf(path, n), _buf(n_path, batch),
-                                _ws(workspace), workspace.nbytes, _stream_on(path, stream)))
+    (batch, max_pages), n, dev = page_table.shape, path.shape[0], _device(page_table)
+    _check(lib().kv_tree_commit(_handles(pools, dev), len(pools), batch, _buf(page_table, batch * max_pages, dev),
+                                max_pages, _buf(seq_lens, batch, dev), _buf(cu_q, batch + 1, dev), n,
+                                _buf(path, n, dev), _buf(n_path, batch, dev), _ws(workspace, dev), workspace.nbytes,
+                                _stream_on(dev, stream)))
 
 
 def moe_forward_workspace_size(shape, max_tokens) -> int:
@@ -459,16 +481,16 @@ def decode_layer_tree(shape, weights: DeviceWeights, pool: KVPool, page_table, s
                       workspace=None, stream=None):
     """decode_layer where each sequence's new tokens are a tree of drafted tokens."""
     hs, hc, batch, max_pages = _tree_batch(page_table, host_seq_lens, host_cu_q)
-    n = hc.item(batch)
-    _check(lib().decode_layer_tree(_cfg_for(shape, pool), ctypes.byref(weights.struct), pool.handle, batch,
-                                   _buf(page_table, batch * max_pages), max_pages, _buf(seq_lens, batch),
-                                   _buf(cu_q, batch + 1), _buf(parents, n), _host(hs), _host(hc),
-                                   _buf(x_in, n * shape.hidden, torch.float32),
-                                   _buf(x_out, n * shape.hidden, torch.float32),
-                                   None if topk_idx is None else _buf(topk_idx, n * shape.top_k),
-                                   None if topk_w is None else _buf(topk_w, n * shape.top_k, torch.float32),
-                                   ctypes.byref(taps) if taps is not None else None, _ws(workspace),
-                                   workspace.nbytes, _stream_on(x_in, stream)))
+    n, dev = hc.item(batch), _device(x_in)
+    _check(lib().decode_layer_tree(_cfg_for(shape, pool), ctypes.byref(weights.struct), _pool(pool, dev), batch,
+                                   _buf(page_table, batch * max_pages, dev), max_pages, _buf(seq_lens, batch, dev),
+                                   _buf(cu_q, batch + 1, dev), _buf(parents, n, dev), _host(hs), _host(hc),
+                                   _buf(x_in, n * shape.hidden, dev, torch.float32),
+                                   _buf(x_out, n * shape.hidden, dev, torch.float32),
+                                   None if topk_idx is None else _buf(topk_idx, n * shape.top_k, dev),
+                                   None if topk_w is None else _buf(topk_w, n * shape.top_k, dev, torch.float32),
+                                   ctypes.byref(taps) if taps is not None else None, _ws(workspace, dev),
+                                   workspace.nbytes, _stream_on(dev, stream)))
 
 
 def decode_layer_noalloc(shape, weights: DeviceWeights, pool: KVPool, page_table, seq_lens, cu_q, host_seq_lens,

@@ -296,3 +296,85 @@ def test_engine_refuses_drafts_that_no_tree_holds():
     for bad in (-1, mcpu.TREE_MAX_NODES):
         with pytest.raises(ValueError):
             rollout.Engine(None, draft_nodes=bad)
+
+
+def test_every_tensor_lies_on_the_calls_device(monkeypatch):
+    """Stand-ins on GPUs 0 and 1, the current one being 0: no call is made with one argument on the other GPU."""
+    made = []
+
+    class Calls:
+        def __getattr__(self, name):
+            return lambda *a: made.append(name) or mcpu.MCPU_OK
+
+    class Tensor:
+        def __init__(self, *shape, dtype=torch.int32, dev=0):
+            self.shape, self.dtype, self.dev = torch.Size(shape), dtype, dev
+            self.device, self.is_cuda, self.nbytes = torch.device("cuda", dev), True, 4 * self.shape.numel()
+
+        def numel(self):
+            return self.shape.numel()
+
+        def get_device(self):
+            return self.dev
+
+        is_contiguous = lambda self: True  # noqa: E731
+        stride = lambda self: ()           # noqa: E731
+        data_ptr = lambda self: D          # noqa: E731
+
+    class Stream:
+        def __init__(self, dev):
+            self.device_index, self.cuda_stream = dev, 0
+
+    monkeypatch.setattr(mcpu, "lib", Calls)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 0, raising=False)
+    s, n = W.TINY, 4
+    f32 = dict(dtype=torch.float32)
+
+    def pool(dev=0):
+        p = object.__new__(mcpu.KVPool)
+        p.shape, p.cfg, p.handle, p.device = s, mcpu.make_cfg(s), None, dev
+        p.k = p.v = Tensor(4, **f32, dev=dev)
+        return p
+
+    class Weights:
+        struct = mcpu.LayerWeights()
+
+    q = lambda: Tensor(n, s.n_q_heads * s.head_dim, **f32)  # noqa: E731
+    x = lambda: Tensor(n, s.hidden, **f32)                  # noqa: E731
+    ws, hs, hc = (lambda: Tensor(4096)), _i32(5, 17), _i32(0, 3, 4)
+    batch = lambda: [Tensor(2, 8), Tensor(2), Tensor(3)]  # noqa: E731
+    calls = {
+        "tree_attention": lambda: [s, Tensor(s.n_q_heads, **f32), pool(), *batch(), Tensor(n), hs, hc, q(), q(), ws(), Stream(0)],
+        "tree_accept": lambda: [Tensor(3), *[Tensor(n) for _ in range(4)], Tensor(2), Tensor(2), ws(), Stream(0)],
+        "kv_tree_commit": lambda: [[pool()], *batch(), Tensor(n), Tensor(2), ws(), Stream(0)],
+        "kv_pages_copy": lambda: [[pool()], Tensor(2), Tensor(2), hs, hs, ws(), Stream(0)],
+        "decode_layer_tree": lambda: [s, Weights, pool(), *batch(), Tensor(n), hs, hc, x(), x(), Tensor(n, s.top_k),
+                                      Tensor(n, s.top_k, **f32), None, ws(), Stream(0)],
+    }
+    for name, args in calls.items():
+        getattr(mcpu, name)(*args())
+        assert made == [name]
+        for i, a in enumerate(args()):
+            if not isinstance(a, (Tensor, mcpu.KVPool, Stream, list)):
+                continue
+            bad = args()
+            if isinstance(a, list):
+                bad[i] = [pool(), pool(1)]
+            elif isinstance(a, Stream):
+                bad[i] = Stream(1)
+            elif isinstance(a, mcpu.KVPool):
+                bad[i] = pool(1)
+            else:
+                bad[i].dev = 1
+            with pytest.raises(mcpu.McpuError):
+                getattr(mcpu, name)(*bad)
+        assert made == [name], i
+        made.clear()
+
+
+def test_missing_host_copies_are_refused():
+    i = lambda *v: torch.tensor(v, dtype=torch.int32)  # noqa: E731
+    for hs, hc in ((None, _i32(0, 1)), (_i32(3), None)):
+        with pytest.raises(mcpu.McpuError):
+            mcpu.tree_attention(W.TINY, None, None, i(0).view(1, 1), i(3), i(0, 1), i(-1), hs, hc, None, None, None)
