@@ -275,6 +275,9 @@ int kv_pages_append(mcpu_kv_pool* pool, int32_t batch, const int32_t* page_table
  *    o_h = sum_j e^{z_j - M} v_j / (e^{s_h - M} + sum_j e^{z_j - M}),
  *    z_j = q_h . k_j / sqrt(d), M = max(s_h, max_j z_j), s_h = sinks[h],
  *  with query head h reading KV head h / (Hq / Hkv). sinks may be NULL (no sink).
+ *  Scores, M, sums and accumulators have 32 bits; in a bf16 layer the weights
+ *  e^{z_j - M} are rounded to bf16 (relative 2^-8) for the product with the values,
+ *  whose operand type it is, and summed after that rounding.
  *  host_seq_lens / host_cu_q: host copies of the same arrays, used only to
  *  plan the launch (no device-to-host traffic). A sequence that adds 16 or
  *  more rows in the step (a tool observation appended as a prefill chunk,
@@ -293,8 +296,9 @@ int paged_attention(const mcpu_layer_cfg* cfg, const float* sinks, mcpu_kv_pool*
  * Run stage's generation (Sec. 3.2): they form a tree whose nodes are the new
  * tokens of the step. A draw depends only on (seed, sequence, position)
  * (lm_head_sample), so the drafted tokens that equal the draws of the tokens
- * before them are exactly the tokens that a token-by-token step would have
- * produced.
+ * before them are the tokens that token-by-token steps would have produced. Steps
+ * of other row counts round differently, so where two ids' perturbed scores lie
+ * within that rounding of each other, the draws may differ.
  *
  * The tree of sequence b is the rows cu_q[b] .. cu_q[b + 1] - 1 of the step: n =
  * 0 to MCPU_TREE_MAX_NODES nodes. Node i's K and V are written to cache position

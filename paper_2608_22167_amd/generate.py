@@ -25,7 +25,8 @@ once, `fork()` gives every member the whole pages and a copy of the last, partly
 filled one. `step_tree()` verifies drafted tokens: where a drafted token equals the
 draw before it, the step yields more than one token per sequence, and because a
 draw depends only on (seed, sequence, position) they are the tokens that `step()`
-would have drawn one by one. `Lookup` drafts from the sequence's own history.
+would have drawn one by one, but where two ids nearly tie: steps of other row counts
+round differently. `Lookup` drafts from the sequence's own history.
 """
 from __future__ import annotations
 
@@ -398,7 +399,8 @@ class Generator:
         TREE_MAX_NODES - 1 of them, none for a sequence without a draft.
         Returns {sid: [(token, logprob), ...]}: the draws along the confirmed
         path, one at least, of which the last becomes the pending token. They
-        are the tokens that calls of `step()` would have drawn. Sequences with
+        are the tokens that calls of `step()` would have drawn, outside near ties
+        (the scores of two ids within the rounding of a step). Sequences with
         longer input are left to `step()`; no more rows are fed than
         max_tokens_per_step, oldest sequences first and drafts only where every
         sequence has its row. A draft for which there are no rows or pages left, or

@@ -80,7 +80,8 @@ class Engine:
     fed before the sequence's next input, so turns join seamlessly. With
     draft_nodes > 0, steps in which every sequence decodes verify that many tokens
     drafted from each sequence's own history (`Generator.step_tree`): the same
-    tokens in fewer steps."""
+    tokens, outside near ties of two ids, in fewer steps. While any sequence still
+    has longer input to feed, steps are plain ones."""
 
     def __init__(self, gen, draft_nodes: int = 0):
         if not 0 <= draft_nodes < TREE_MAX_NODES:
