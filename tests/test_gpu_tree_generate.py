@@ -387,3 +387,27 @@ def test_engine_drafts_from_history():
     finally:
         eng.close()
     assert gen.free_pages() == free0
+
+
+def test_layer_over_trees_with_native_mxfp4_experts():
+    """The layer's feed-forward half on the residual that its attention left is moe_forward's, bit for bit, and the
+    attention half is that of the same trees' branches (here chains) in decode_layer."""
+    shape = replace(W.GPT_OSS_20B, expert_fmt="mxfp4_native", n_experts=4, top_k=2, hidden=256, ffn_dim=256,
+                    n_q_heads=16, n_kv_heads=2)
+    rng = np.random.default_rng(52)
+    seq = np.array([33, 90, 5], np.int32)
+    for tr in ([R.random_tree(rng, 12, 3), [-1], R.random_tree(rng, 40, 4)], [[i - 1 for i in range(k)] for k in (12, 1, 15)]):
+        wl = W.custom(shape, seq, np.array([len(t) for t in tr]), 1306, sink_std=0.5)
+        par = np.array([p for t in tr for p in t], np.int32)
+        weights = mcpu.DeviceWeights(shape, wl.weights)
+        args = (wl, weights, wl.k_pool.cuda(), wl.v_pool.cuda(), seq, wl.cu_q, wl.x_in.cuda(), wl.page_table)
+        o, h1, out, k, v = _layer(*args, par)
+        want = torch.empty_like(out)
+        ws = mcpu.workspace(mcpu.moe_forward_workspace_size(shape, len(par)))
+        mcpu.moe_forward(shape, weights, h1, want, workspace=ws)
+        assert mcpu.mcpu_check_device_errors(ws) == 0
+        assert torch.equal(out, want)
+    b = _layer(*args)
+    PT.check("o", o.float().cpu(), b[0].float().cpu(), "bf16")
+    PT.check("h1", h1.cpu(), b[1].cpu(), "bf16")
+    assert torch.equal(k, b[3]) and torch.equal(v, b[4])
