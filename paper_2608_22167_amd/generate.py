@@ -280,19 +280,23 @@ class Generator:
         except mcpu.McpuError as e:
             if e.code != mcpu.MCPU_ENOMEM:
                 raise
-            self._trim(s, s.length + 1)
+            self._trim([s], 1)
             return False
         return True
 
-    def _trim(self, s: _Seq, n: int) -> None:
-        """Free the pages behind position n - 1, which drafted tokens that did not stay have taken."""
-        keep = (n + PAGE - 1) // PAGE
-        if len(s.pages_full) > keep:
-            mcpu.kv_pages_free(self.alloc_full, np.array(s.pages_full[keep:], np.int32))
+    def _trim(self, seqs: Sequence[_Seq], more: int = 0) -> None:
+        """Free the pages behind position s.length + more - 1 of each sequence, which drafted tokens that did not
+        stay have taken. One call for each kind: sequence by sequence a step of 48 trees took 0.15-0.2 ms more."""
+        full: List[int] = []
+        window: List[int] = []
+        for s in seqs:
+            keep = (s.length + more + PAGE - 1) // PAGE
+            full += s.pages_full[keep:]
             del s.pages_full[keep:]
-        behind = [lp for lp in s.pages_sw if lp >= keep]
-        if behind:
-            mcpu.kv_pages_free(self.alloc_sw, np.array([s.pages_sw.pop(lp) for lp in behind], np.int32))
+            window += [s.pages_sw.pop(lp) for lp in [lp for lp in s.pages_sw if lp >= keep]]
+        for alloc, pages in ((self.alloc_full, full), (self.alloc_sw, window)):
+            if pages:
+                mcpu.kv_pages_free(alloc, np.array(pages, np.int32))
 
     def _shrink(self, s: _Seq) -> None:
         """Free window pages wholly left of the next token's window."""
@@ -421,8 +425,7 @@ class Generator:
         try:
             return self._step_trees(trees)
         finally:
-            for s, *_ in trees:
-                self._trim(s, s.length)
+            self._trim([s for s, *_ in trees])
 
     def _step_trees(self, trees) -> Dict[int, List[tuple]]:
         """step_tree of checked drafts: (sequence, tokens, parents, depths from the pending token on)."""
