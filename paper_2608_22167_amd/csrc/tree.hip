@@ -498,10 +498,12 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(TreeAttn P, int tiles) {
 // The maximum of a column is raised only when a lane's share of a step's weights
 // would pass 2^8, so that most steps have no cross-lane step and no rescale.
 //
-// Wide trees are bound by the vector pipe beside the products: 16 trees of 33-64 nodes
-// behind 8-16 K tokens take 192 us with the combine (650 TFLOP/s over the pairs in
-// sight); without loads and barriers the same instructions take 85% of that. Narrow
-// trees are bound by HBM.
+// Wide trees are bound by no unit alone: 16 trees of 33-64 nodes (7.6 M node and key
+// pairs a head) take 192 us with the combine, 650 TFLOP/s. Of its wavefronts' cycles 39%
+// have an instruction at work, 34% wait for loads and at barriers, 27% for their turn or
+// a result; the matrix cores are busy 30% of the launch, the vector pipe 40%. 18% of the
+// wavefronts' steps have no columns (a tree's last column tile), and 992 workgroups on
+// 512 places are two uneven rounds. Narrow trees are bound by HBM.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) void* lds_void_t;
@@ -1080,22 +1082,24 @@ __global__ __launch_bounds__(64, 3) void tree_attn_narrow_kernel(TreeAttn P, int
 // the step's pages fit the caches and its splits leave compute units idle; `one_each`:
 // no tree is split. Latency bounds such steps, and bandwidth or the vector pipe the
 // rest. Streaming loads serve pages that one wavefront or workgroup reads, once; with
-// several column tiles they make each fetch its pages anew. Measured in us, 64 query
-// heads on 8 KV heads, six sets of pools in turn (contexts of 4-16 K tokens unless
-// given; NARROW2 was NARROW_STREAM with two column tiles a wavefront):
+// several column tiles they make each fetch its pages anew. Measured in us by events
+// around the launch, 64 query heads on 8 KV heads, six sets of pools in turn, contexts
+// of 4-16 K tokens unless given (one draw of the sizes for all forms, not the one of the
+// figures at the kernels: the 16 wide trees here have 5.3 M pairs). NARROW2 was
+// NARROW_STREAM with two column tiles a wavefront, measured on an earlier build.
 //   up to 32 columns, 256 windowed trees of 1-4 nodes: NARROW_STREAM 18.5, NARROW 21.8; 48 trees of 1-4
-//     NARROW_STREAM 102, NARROW 115, WIDE2 107; one tree of 4 behind 6 K NARROW 8.9, WIDE1 9.6
-//   few or one each, up to 96: 256 windowed trees of 2-12 NARROW 32, NARROW_STREAM 32.5, WIDE2 34, WIDE1 36; one
-//     tree of 8 behind 6 K NARROW 9.8, WIDE1 10.5
-//   few or one each, above: 256 windowed trees of 8-16 WIDE1 and WIDE2 41, NARROW 45; one tree of 16 behind 6 K
-//     WIDE1 11.8, NARROW 12.0, WIDE2 13.8, of 64 WIDE1 21.6, NARROW 22.2, WIDE4 23.2; 16 windowed trees of 17-30
-//     NARROW 10.8, WIDE1 11.2, WIDE4 14.2
-//   up to 128, 48 trees of 1-8: WIDE2 113 + 5 for the combine, NARROW2 108 + 9, NARROW 162; 128 trees of 1-8 WIDE2
-//     311 + 9, NARROW2 303 + 13; 24 trees of 1-8 WIDE2 50 + 6, NARROW2 53 + 8; 48 trees of 8-16 WIDE2 121, WIDE1 128,
-//     WIDE4 162
-//   above, 24 trees of 16-32: WIDE4 137, WIDE1 144, WIDE2 152; 16 of 33-64 behind 8-16 K WIDE4 164, WIDE1 164 and 3
-//     more in the combine, WIDE2 185; one workgroup of eight wavefronts for 512 columns was 10-20% slower than two of
-//     WIDE4, whose barriers stop fewer wavefronts
+//     NARROW_STREAM 102, NARROW 114, WIDE2 108; one tree of 4 behind 6 K NARROW 9.0, WIDE1 9.8
+//   few or one each, up to 96: 256 windowed trees of 2-12 NARROW 32.3, NARROW_STREAM 33.8, WIDE2 34.8, WIDE1 36.2;
+//     one tree of 8 behind 6 K NARROW 9.9, WIDE1 10.3
+//   few or one each, above: 256 windowed trees of 8-16 WIDE1 40.8, WIDE2 41.7, NARROW 45; one tree of 16 behind 6 K
+//     WIDE1 11.9, NARROW 12.1, WIDE2 14.0, of 64 WIDE1 21.6, NARROW 22.3, WIDE4 23.4; 16 windowed trees of 17-30
+//     WIDE1 11.0, NARROW 11.4, WIDE4 14.6
+//   up to 128, 48 trees of 1-8: WIDE2 109 + 5 for the combine, NARROW2 108 + 9, NARROW 156; 128 trees of 1-8 WIDE2
+//     308 + 6, NARROW2 303 + 13; 24 trees of 1-8 WIDE2 49 + 6, NARROW2 53 + 8, NARROW 56; 48 trees of 8-16 WIDE1
+//     122-125 + 16, WIDE2 124-129 + 8, WIDE4 154-159 + 8
+//   above, 24 trees of 16-32: WIDE4 139 + 7, WIDE1 135-145 + 9, WIDE2 153-156 + 7; 16 of 33-64 behind 8-16 K WIDE4
+//     163-167 + 7, WIDE1 160-163 + 9, WIDE2 187-193 + 7; one workgroup of eight wavefronts for 512 columns was 10-20%
+//     slower than two of WIDE4, whose barriers stop fewer wavefronts
 TreeForm tree_attn_form(int dtype, int head_dim, const void* k_pool, const void* v_pool, int cols, bool few, bool one_each) {
   if (dtype != 1 || head_dim != 64 || ((uintptr_t)k_pool | (uintptr_t)v_pool) % 16) return {TREE_ANY, 16, 12};
   if (cols <= 32) return {few ? TREE_NARROW : TREE_NARROW_STREAM, 32, 8};
@@ -1138,8 +1142,8 @@ hipError_t launch_tree_attn(int dtype, int head_dim, const TreeAttn& p, hipStrea
 // lane group per pair, which goes through its splits four at a time, or, with many
 // splits or few pairs (MANY), the whole wavefront, its lane groups joined at the end.
 // Bound by three rounds of latency, then by HBM: 31 splits of one tree 4.8 us (MANY); up
-// to four splits of 16 trees of 33-64 nodes 7.4 us (MANY 12.2, more than half of it
-// vector work of the joins), of 48 trees of 1-8 5.5 (MANY 5.1).
+// to four splits of 16 trees of 33-64 nodes, 20 MB of rows, 7.4 us (MANY 12.2, more than
+// half of it vector work of the joins), up to six, 52 MB, 11 us; 48 trees of 1-8 5.5 (MANY 5.1).
 template <typename T, int D, bool MANY>
 __global__ __launch_bounds__(256) void tree_combine_kernel(TreeCombine P) {
   constexpr int LR = D / 4, RW = 64 / LR, STEP = MANY ? RW : 1;
