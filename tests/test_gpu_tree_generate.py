@@ -411,3 +411,23 @@ def test_layer_over_trees_with_native_mxfp4_experts():
     PT.check("o", o.float().cpu(), b[0].float().cpu(), "bf16")
     PT.check("h1", h1.cpu(), b[1].cpu(), "bf16")
     assert torch.equal(k, b[3]) and torch.equal(v, b[4])
+
+
+def test_layer_over_trees_with_empty_trees():
+    """Sequences without nodes at either end and in between change no bit of the others."""
+    shape = replace(W.GPT_OSS_20B, n_q_heads=16, n_kv_heads=2, hidden=256, ffn_dim=256, n_experts=4, top_k=2)
+    rng = np.random.default_rng(53)
+    tr = [R.random_tree(rng, 9, 3), R.random_tree(rng, 30, 4)]
+    seq, n = np.array([40, 700], np.int32), np.array([9, 30])
+    wl = W.custom(shape, seq, n, 1307, sink_std=0.5)
+    par = np.array([p for t in tr for p in t], np.int32)
+    weights = mcpu.DeviceWeights(shape, wl.weights)
+    pools_x = wl.k_pool.cuda(), wl.v_pool.cuda()
+    a = _layer(wl, weights, *pools_x, seq, wl.cu_q, wl.x_in.cuda(), wl.page_table, par)
+    rows = [0, 0, 1, 1, 1]
+    table = wl.page_table[rows].copy()
+    table[[0, 2, 4]] = -1
+    cu = np.array([0, 0, 9, 9, 39, 39], np.int32)
+    b = _layer(wl, weights, *pools_x, np.array([5, 40, 0, 700, 9000], np.int32), cu, wl.x_in.cuda(), table, par)
+    for x, y in zip(a, b):
+        assert torch.equal(x, y)
