@@ -267,6 +267,7 @@ class DeviceWeights:
     def __init__(self, shape, W, device="cuda", pack=True):
         self.t = {k: v.to(device).contiguous() for k, v in W.items()}
         t = self.t
+        self.device = next(iter(t.values())).get_device()
         mx = shape.expert_fmt != "dense"
         if pack and not mx and shape.dtype == "bf16" and shape.hidden % 64 == 0 and shape.ffn_dim % 64 == 0:
             t["w_gu_packed"] = packed_weights(t["w_gu"])
@@ -482,6 +483,8 @@ def decode_layer_tree(shape, weights: DeviceWeights, pool: KVPool, page_table, s
     """decode_layer where each sequence's new tokens are a tree of drafted tokens."""
     hs, hc, batch, max_pages = _tree_batch(page_table, host_seq_lens, host_cu_q)
     n, dev = hc.item(batch), _device(x_in)
+    if weights.device != dev:
+        raise McpuError(MCPU_EINVAL, f"the weights lie on GPU {weights.device}, the call's is {dev}")
     _check(lib().decode_layer_tree(_cfg_for(shape, pool), ctypes.byref(weights.struct), _pool(pool, dev), batch,
                                    _buf(page_table, batch * max_pages, dev), max_pages, _buf(seq_lens, batch, dev),
                                    _buf(cu_q, batch + 1, dev), _buf(parents, n, dev), _host(hs), _host(hc),

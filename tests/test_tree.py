@@ -340,6 +340,9 @@ def test_every_tensor_lies_on_the_calls_device(monkeypatch):
     class Weights:
         struct = mcpu.LayerWeights()
 
+        def __init__(self, dev=0):
+            self.device = dev
+
     q = lambda: Tensor(n, s.n_q_heads * s.head_dim, **f32)  # noqa: E731
     x = lambda: Tensor(n, s.hidden, **f32)                  # noqa: E731
     ws, hs, hc = (lambda: Tensor(4096)), _i32(5, 17), _i32(0, 3, 4)
@@ -349,20 +352,20 @@ def test_every_tensor_lies_on_the_calls_device(monkeypatch):
         "tree_accept": lambda: [Tensor(3), *[Tensor(n) for _ in range(4)], Tensor(2), Tensor(2), ws(), Stream(0)],
         "kv_tree_commit": lambda: [[pool()], *batch(), Tensor(n), Tensor(2), ws(), Stream(0)],
         "kv_pages_copy": lambda: [[pool()], Tensor(2), Tensor(2), hs, hs, ws(), Stream(0)],
-        "decode_layer_tree": lambda: [s, Weights, pool(), *batch(), Tensor(n), hs, hc, x(), x(), Tensor(n, s.top_k),
+        "decode_layer_tree": lambda: [s, Weights(), pool(), *batch(), Tensor(n), hs, hc, x(), x(), Tensor(n, s.top_k),
                                       Tensor(n, s.top_k, **f32), None, ws(), Stream(0)],
     }
     for name, args in calls.items():
         getattr(mcpu, name)(*args())
         assert made == [name]
         for i, a in enumerate(args()):
-            if not isinstance(a, (Tensor, mcpu.KVPool, Stream, list)):
+            if not isinstance(a, (Tensor, mcpu.KVPool, Weights, Stream, list)):
                 continue
             bad = args()
             if isinstance(a, list):
                 bad[i] = [pool(), pool(1)]
-            elif isinstance(a, Stream):
-                bad[i] = Stream(1)
+            elif isinstance(a, (Stream, Weights)):
+                bad[i] = type(a)(1)
             elif isinstance(a, mcpu.KVPool):
                 bad[i] = pool(1)
             else:
