@@ -312,9 +312,9 @@ enum { MCPU_TREE_MAX_NODES = 64 };
  * committed keys and to its ancestors and itself, in a window w > 0 to those of
  * them at positions above p_i - w. Formula, sinks, types and layouts as for
  * paged_attention; a node whose keys all lie on missing pages gives zeros, also
- * with a sink of -inf, which is as none. Cache contents that no node of the tree sees (slots behind
- * the tree, stale ones, other branches) have no effect on a node, whatever they
- * hold.
+ * with a sink of -inf, which is as none. Cache contents that no node of the tree
+ * sees (slots behind the tree, stale ones, other branches) have no effect on a
+ * node, whatever they hold.
  *  cu_q (device) and host_cu_q are required, as are host_seq_lens; parents:
  *  device int32 [n_tokens]. Each tree has up to MCPU_TREE_MAX_NODES nodes, else
  *  MCPU_EUNSUPPORTED. Rows of q and o outside the trees do not exist.

@@ -9,9 +9,9 @@ namespace mcpu {
 constexpr int TREE_MAX_NODES = 64;  // a node's ancestors are the bits of one 64-bit word
 
 // One split of a tree's visible pages: n nodes (rows t0 ..) of sequence b (-1: no
-// split) behind len committed tokens, logical pages pg0 .. pg1 - 1. Its partial rows (node i of
-// part_ml / part_acc at row0 + i) exist where the tree has more than one split; a
-// tree's only split writes o itself.
+// split) behind len committed tokens, logical pages pg0 .. pg1 - 1. Its partial rows
+// (node i of part_ml / part_acc at row0 + i) exist where the tree has more than one
+// split; a tree's only split writes o itself.
 struct TreeItem {
   int32_t b, t0, n, len, pg0, pg1, row0, splits;
 };
